@@ -348,6 +348,109 @@ int cass_accept_sampling(void* session, int n_seq, const int32_t* draft, int dra
 int cass_softmax(const float* logits, int rows, int vocab, float temperature, float* probs, void* stream);
 int cass_sample(const float* probs, int rows, int vocab, const float* u, int32_t* tokens, int tok_stride, void* stream);
 
+/* ------------------------------------------------------------------------------------------------------
+ * Operators of a serving loop on bf16 / fp16 caches in the caller's own layout: rotary positions, attention of a
+ * batch that shares a prefix, eviction from a cache.  They need no session.  Strides count elements; the
+ * innermost dimension (a head's values) is contiguous.
+ * ---------------------------------------------------------------------------------------------------- */
+enum { CASS_BF16 = 0, CASS_F16 = 1, CASS_F32 = 2 };
+
+/* Rotary positions.  A head's first rot_dim values form rot_dim / 2 pairs; pair j of a row at position p is turned by
+ * the angle p * f_j, f_j = theta^(-2j / rot_dim) scaled for contexts longer than the model was trained on:
+ *   CASS_ROPE_PLAIN   f_j
+ *   CASS_ROPE_LINEAR  f_j / factor
+ *   CASS_ROPE_NTK     f_j of theta * factor^(rot_dim / (rot_dim - 2))                                 (rot_dim > 2)
+ *   CASS_ROPE_BANDS   by the turns that pair j makes over trained_len positions, u_j = trained_len f_j / 2 pi: up to `low`
+ *                     f_j / factor, from `high` on f_j, between them m f_j + (1 - m) f_j / factor with
+ *                     m = (u_j - low) / (high - low)                                               (0 < low < high)
+ *   CASS_ROPE_YARN    with c(u) = rot_dim ln(trained_len / (2 pi u)) / (2 ln theta), a = max(floor(c(high)), 0),
+ *                     b = min(ceil(c(low)), rot_dim - 1), m_j = clamp((j - a) / max(b - a, 0.001), 0, 1):
+ *                     m_j f_j / factor + (1 - m_j) f_j; sines and cosines are multiplied by `gain`  (0 < low < high)
+ * gain: 0 takes 0.1 ln(factor) + 1 for CASS_ROPE_YARN (1 for factor <= 1) and 1 for the others; another positive value is taken as it is. */
+enum { CASS_ROPE_PLAIN = 0, CASS_ROPE_LINEAR = 1, CASS_ROPE_NTK = 2, CASS_ROPE_BANDS = 3, CASS_ROPE_YARN = 4 };
+typedef struct cass_rope_params {
+    int rot_dim, scaling;
+    double theta, factor, low, high, trained_len, gain;     /* theta > 1; what the scaling does not use is ignored */
+} cass_rope_params;
+
+/* freqs: device, rot_dim / 2 + 1 doubles, 8-byte aligned: the f_j, then the factor on sines and cosines.  A program computes
+ * them once a model. */
+int cass_rope_freqs(const cass_rope_params* params, double* freqs, void* stream);
+
+/* Rotary positions of the session by `params` (see cass_rope_params; rot_dim = head_dim) instead of rope_theta unscaled: the tables that
+ * prefill, draft and verification read are written anew.  For a session without positions in its caches (after cass_session_init or
+ * cass_session_reset): rotated keys stay as they are.  Work on `stream` that was enqueued earlier still reads the old tables. */
+int cass_session_set_rope(void* session, const cass_rope_params* params, void* stream);
+
+/* Queries and keys of `rows` rows: (row, head) of q begins q_row * row + q_head * head elements behind q, and so on.  A head's
+ * pairs are (j, j + rot_dim/2), or (2j, 2j + 1) with `interleaved`.  dtype: CASS_BF16, CASS_F16 or CASS_F32, one for all. */
+typedef struct cass_rope_geom {
+    int dtype, head_dim, rot_dim, interleaved, n_q_heads, n_k_heads;
+    int64_t q_row, q_head, k_row, k_head, q_out_row, q_out_head, k_out_row, k_out_head;
+} cass_rope_geom;
+
+/* Turns every pair (a, b) of row r's heads by t = positions[r] * f_j: (g (a cos t - b sin t), g (a sin t + b cos t)), g the factor
+ * behind the frequencies; values beyond rot_dim are copied.  transpose: by -t, which is the gradient of the forward call's
+ * inputs from that of its outputs and, for g = 1, undoes the rotation.  Angles are formed in 64 bits (any int32 position), the
+ * products in 32, one rounding at the end.  positions: device int32 [rows], or NULL for 0, 1, 2, ...  k may be NULL
+ * (n_k_heads = 0), and q likewise.  q_out = q with the same strides rotates in place (k likewise); outputs overlap neither
+ * each other nor inputs otherwise.  The elements of one output must not overlap (CASS_ERR_INVALID_ARG).  rows = 0 does nothing.
+ * Calls for rows x heads up to 2^31 - 1. */
+int cass_rope(const cass_rope_geom* geom, const double* freqs, const int32_t* positions, int rows, const void* q, const void* k,
+              void* q_out, void* k_out, int transpose, void* stream);
+
+/* A batch's K (or V) cache: value c of (sequence, position, head) lies seq_stride * sequence + pos_stride * position +
+ * head_stride * head + c elements behind the pointer.  K and V have the same layout.  dtype: CASS_BF16 or CASS_F16.  Pointers
+ * are 16-byte aligned, the strides multiples of 8, and no two rows overlap (CASS_ERR_INVALID_ARG).
+ * capacity: positions of a sequence that there is room for. */
+typedef struct cass_cache_geom {
+    int dtype, n_seq, n_kv_heads, head_dim, capacity;
+    int64_t seq_stride, pos_stride, head_stride;
+} cass_cache_geom;
+
+/* Grouped-query attention of `rows` new rows of every sequence (1 to 16) over a prefix that all sequences share, read once
+ * for all of them, and each sequence's own cache.  K of both is post-RoPE.  With lens[b] the positions in sequence b's cache,
+ * the new rows' among them, row r sees the whole prefix and the first lens[b] - (rows - 1 - r) positions of its cache:
+ *   s = scale q.k;  out = sum_j softmax(s)_j v_j;  lse = ln sum_j e^{s_j}  (-inf, and out 0, for a row that sees nothing)
+ * What a row does not see does not reach its results, whatever its bits.  A sequence with lens[b] < 0 is not there: nothing
+ * of it is read or written.  A length beyond the capacity is cut to it, and d_status receives CASS_ERR_CAPACITY.
+ * weight_out (optional): fp32 [n_seq][n_kv_heads][capacity] = weight_in (NULL: 0) + the attention weights that each position of
+ * the sequence's own cache got in this call, summed over rows and the group's query heads: what cass_kv_evict goes by.
+ * weight_out = weight_in adds in place.
+ * q, out: dtype of the cache, 16-byte aligned, strides multiples of 8.  lse (optional): fp32 [n_seq][rows][n_q_heads].
+ * prefix_len = 0 (pointers NULL) or capacity = 0 (pointers and lens NULL: every row sees the prefix alone) leave a part out.
+ * head_dim 32, 64, 96, 128, 192 or 256; at most 16 query heads a KV head; n_seq up to 4096; CASS_ERR_UNSUPPORTED otherwise.
+ * Probabilities are rounded to the cache's type for the second product, sums are 32 bits.  Results are the same bits
+ * on every call with the same inputs and sizes.  scratch: device, 16-byte aligned, of cass_shared_prefix_scratch_bytes; two calls
+ * that may overlap on the GPU need their own.  d_status (required): device int32, left alone if nothing went wrong. */
+typedef struct cass_shared_attn {
+    int n_q_heads, rows;
+    int64_t q_seq, q_row, q_head, out_seq, out_row, out_head;
+    int prefix_len;
+    int64_t prefix_pos_stride, prefix_head_stride;
+    float scale;                /* 0: 1 / sqrt(head_dim) */
+} cass_shared_attn;
+size_t cass_shared_prefix_scratch_bytes(const cass_cache_geom* cache, const cass_shared_attn* attn, int with_weights);   /* 0: bad arguments */
+int cass_shared_prefix_attention(const cass_cache_geom* cache, const cass_shared_attn* attn, const void* q, const void* k_prefix,
+                                 const void* v_prefix, const void* k_cache, const void* v_cache, const int32_t* lens, void* out, float* lse,
+                                 const float* weight_in, float* weight_out, void* scratch, size_t scratch_bytes, int32_t* d_status,
+                                 void* stream);
+
+/* Eviction.  Of every (sequence, KV head) with more than `budget` positions the first n_first stay, the last n_last, and of
+ * those between them the budget - n_first - n_last with the largest weight (ties: the lower position; -0 = +0; NaN below all);
+ * a cache of at most `budget` positions keeps all.  What stays moves to the front, in order.
+ * weight: fp32 [n_seq][n_kv_heads][capacity]; lens: int32 [n_seq].  kept: int32 [n_seq][n_kv_heads][budget], the positions that
+ * stay, ascending, then -1; new_lens: int32 [n_seq] = min(lens, budget), may be lens.  cache_out NULL: in place (k_out and v_out
+ * NULL too); otherwise K and V go to another cache of the same type, heads and sequences and a capacity of at least
+ * `budget`, which must not overlap the first.  weight_out (optional, may be `weight` in place): fp32 [n_seq][n_kv_heads]
+ * [capacity of the output], the weights of what stays, then zeros up to the capacity.  Rows of K and V behind what stays are left as
+ * they were.  A sequence whose length is outside 0 .. capacity is left alone: its `kept` is -1, its new_lens its length, its
+ * caches and weights are not written.
+ * 1 <= budget <= capacity (of the output); n_first, n_last >= 0, n_first + n_last <= budget.  head_dim a multiple of 8, at most 512. */
+int cass_kv_evict(const cass_cache_geom* cache, void* k_cache, void* v_cache, const float* weight, const int32_t* lens, int budget,
+                  int n_first, int n_last, const cass_cache_geom* cache_out, void* k_out, void* v_out, float* weight_out, int32_t* kept,
+                  int32_t* new_lens, void* stream);
+
 /* Geometry of the compressed KV cache of (sequence, layer, kind 0=K 1=V, head) for tests: device pointers to the
  * fixed-part blocks, the unary arena and the per-token word offsets, plus words per token in the fixed part. */
 typedef struct cass_kv_view {

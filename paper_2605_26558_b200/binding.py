@@ -16,6 +16,8 @@ LIB_PATH = os.path.join(_HERE, "libcass.so")
 
 OK, ERR_INVALID_ARG, ERR_CAPACITY, ERR_UNSUPPORTED, ERR_TIMEOUT, ERR_CUDA = 0, -1, -2, -3, -4, -5
 KV_BF16, KV_COMPRESSED = 1, 2
+BF16, F16, F32 = 0, 1, 2
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_BANDS, ROPE_YARN = 0, 1, 2, 3, 4
 _ERR = {-1: "CASS_ERR_INVALID_ARG", -2: "CASS_ERR_CAPACITY", -3: "CASS_ERR_UNSUPPORTED", -4: "CASS_ERR_TIMEOUT",
         -5: "CASS_ERR_CUDA"}
 
@@ -85,6 +87,26 @@ class KVView(C.Structure):
                 ("arena_words", C.c_int)]
 
 
+class RopeParams(C.Structure):
+    _fields_ = [("rot_dim", C.c_int), ("scaling", C.c_int)] + [(n, C.c_double) for n in ("theta", "factor", "low", "high", "trained_len", "gain")]
+
+
+class RopeGeom(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dtype", "head_dim", "rot_dim", "interleaved", "n_q_heads", "n_k_heads")] + \
+               [(n, C.c_int64) for n in ("q_row", "q_head", "k_row", "k_head", "q_out_row", "q_out_head", "k_out_row", "k_out_head")]
+
+
+class CacheGeom(C.Structure):
+    _fields_ = [(n, C.c_int) for n in ("dtype", "n_seq", "n_kv_heads", "head_dim", "capacity")] + \
+               [(n, C.c_int64) for n in ("seq_stride", "pos_stride", "head_stride")]
+
+
+class SharedAttn(C.Structure):
+    _fields_ = [("n_q_heads", C.c_int), ("rows", C.c_int)] + \
+               [(n, C.c_int64) for n in ("q_seq", "q_row", "q_head", "out_seq", "out_row", "out_head")] + [("prefix_len", C.c_int)] + \
+               [(n, C.c_int64) for n in ("prefix_pos_stride", "prefix_head_stride")] + [("scale", C.c_float)]
+
+
 def _load() -> C.CDLL:
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"{LIB_PATH} is missing: build it with `python -m paper_2605_26558_b200.build` "
@@ -98,6 +120,7 @@ from . import _fastcall  # noqa: E402
 lib.cass_version.restype = C.c_char_p
 lib.cass_verify_gemm_scratch_bytes.restype = C.c_size_t
 lib.cass_verify_from_parts_scratch_bytes.restype = C.c_size_t
+lib.cass_shared_prefix_scratch_bytes.restype = C.c_size_t
 if hasattr(lib, "cass_calib_norms_count"):
     lib.cass_calib_norms_count.restype = C.c_size_t
 
@@ -338,6 +361,45 @@ def cass_sample(probs, rows: int, vocab: int, u, tokens, stream=None, tok_stride
     rc = _fastcall.cass_sample(probs, rows, vocab, u, tokens, tok_stride, stream)
     if rc:
         raise CassError("cass_sample", rc)
+
+
+def cass_rope_freqs(params: RopeParams, freqs, stream=None):
+    rc = _fastcall.cass_rope_freqs(params, freqs, stream)
+    if rc:
+        raise CassError("cass_rope_freqs", rc)
+
+
+def cass_rope(geom: RopeGeom, freqs, positions, rows: int, q, k, q_out, k_out, transpose: int = 0, stream=None):
+    rc = _fastcall.cass_rope(geom, freqs, positions, rows, q, k, q_out, k_out, transpose, stream)
+    if rc:
+        raise CassError("cass_rope", rc)
+
+
+def cass_session_set_rope(session, params: RopeParams, stream=None):
+    _check("cass_session_set_rope", lib.cass_session_set_rope(session, C.byref(params), _stream(stream)))
+
+
+def cass_shared_prefix_scratch_bytes(cache: CacheGeom, attn: SharedAttn, with_weights: bool = False) -> int:
+    n = int(lib.cass_shared_prefix_scratch_bytes(C.byref(cache), C.byref(attn), int(with_weights)))
+    if n == 0:
+        raise CassError("cass_shared_prefix_scratch_bytes", ERR_INVALID_ARG)
+    return n
+
+
+def cass_shared_prefix_attention(cache: CacheGeom, attn: SharedAttn, q, k_prefix, v_prefix, k_cache, v_cache, lens, out, lse, weight_in, weight_out,
+                                 scratch, scratch_bytes: int, d_status, stream=None):
+    rc = _fastcall.cass_shared_prefix_attention(cache, attn, q, k_prefix, v_prefix, k_cache, v_cache, lens, out, lse, weight_in, weight_out, scratch,
+                                                scratch_bytes, d_status, stream)
+    if rc:
+        raise CassError("cass_shared_prefix_attention", rc)
+
+
+def cass_kv_evict(cache: CacheGeom, k_cache, v_cache, weight, lens, budget: int, n_first: int, n_last: int, cache_out, k_out, v_out, weight_out, kept,
+                  new_lens, stream=None):
+    rc = _fastcall.cass_kv_evict(cache, k_cache, v_cache, weight, lens, budget, n_first, n_last, cache_out, k_out, v_out, weight_out, kept, new_lens,
+                                 stream)
+    if rc:
+        raise CassError("cass_kv_evict", rc)
 
 
 def cass_kv_query(session, layer: int, kind: int, head: int, seq: int = 0) -> KVView:

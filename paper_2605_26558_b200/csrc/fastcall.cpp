@@ -80,7 +80,7 @@ bool convert(PyObject* o, T* out) {
         using P = std::remove_cv_t<std::remove_pointer_t<T>>;
         void* p = nullptr;
         bool ok;
-        if constexpr (std::is_class_v<P>) ok = buffer_address(o, sizeof(P), &p);
+        if constexpr (std::is_class_v<P>) ok = (std::is_same_v<P, cass_cache_geom> && o == Py_None) || buffer_address(o, sizeof(P), &p);      // None: in place
         else ok = device_address(o, &p);
         *out = static_cast<T>(p);
         return ok;
@@ -162,7 +162,8 @@ PyObject* stream_address(PyObject*, PyObject* const* a, Py_ssize_t n) {
 PyMethodDef kMethods[] = {
     CASS_ENTRY(cass_draft_gemv), CASS_ENTRY(cass_draft_gemv_batch), CASS_ENTRY(cass_draft_gemv_static), CASS_ENTRY(cass_kv_append),
     CASS_ENTRY(cass_set_len), CASS_ENTRY(cass_draft_step), CASS_ENTRY(cass_verify), CASS_ENTRY(cass_draft_attention), CASS_ENTRY(cass_accept),
-    CASS_ENTRY(cass_accept_sampling), CASS_ENTRY(cass_softmax), CASS_ENTRY(cass_sample),
+    CASS_ENTRY(cass_accept_sampling), CASS_ENTRY(cass_softmax), CASS_ENTRY(cass_sample), CASS_ENTRY(cass_rope_freqs), CASS_ENTRY(cass_rope),
+    CASS_ENTRY(cass_shared_prefix_attention), CASS_ENTRY(cass_kv_evict),
     {"cass_verify_gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&verify_gemm)), METH_FASTCALL, nullptr},
     {"stream_address", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&stream_address)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

@@ -141,8 +141,12 @@ inline Partials draft_gemv_partials(const float* partial, const cass_blob_info& 
     return Partials{partial, bi.n_seg, n_pad, (size_t)bi.n_seg * n_pad};
 }
 
+// Alignment, signs and overlaps of a cache's layout (kv_evict.cu); any: a capacity of 0 is one.
+bool cache_geom_ok(const cass_cache_geom& g, bool any);
+
 // ---- small ops (ops.cu) -------------------------------------------------------------------------------
-int launch_rope_table(float* cos_t, float* sin_t, int max_seq, int d, float theta, cudaStream_t s);
+bool rope_params_ok(const cass_rope_params& p);
+int launch_rope_table(float* cos_t, float* sin_t, int max_seq, const cass_rope_params& p, cudaStream_t s);      // p.rot_dim: the head size
 // row r (the (r % rps)-th of sequence r / rps) takes token toks[(r / rps) * seq_stride + r % rps]
 int launch_embed(const int32_t* toks, int rps, int seq_stride, const uint16_t* embed, uint16_t* h, int rows, int hidden, cudaStream_t s);
 int launch_rmsnorm(const uint16_t* h, const uint16_t* gain, uint16_t* out, int rows, int hidden, float eps,

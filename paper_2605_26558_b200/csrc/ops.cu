@@ -5,16 +5,6 @@
 
 namespace cass {
 
-__global__ void k_rope_table(float* __restrict__ cos_t, float* __restrict__ sin_t, int max_seq, int half, float theta) {
-    size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
-    if (i >= (size_t)max_seq * half) return;
-    int pos = (int)(i / half), j = (int)(i % half);
-    double inv = pow((double)theta, -2.0 * (double)j / (double)(2 * half));
-    double ang = (double)pos * inv;
-    cos_t[i] = (float)cos(ang);
-    sin_t[i] = (float)sin(ang);
-}
-
 __global__ void k_embed(const int32_t* __restrict__ toks, int rps, int seq_stride, const uint16_t* __restrict__ embed,
                         uint16_t* __restrict__ h, int hidden) {
     pdl_wait();
@@ -427,13 +417,6 @@ __global__ void k_calib_accum(const uint16_t* __restrict__ x, int rows, int cols
 __global__ void k_sqrt(const float* __restrict__ in, float* __restrict__ out, size_t n) {
     size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
     if (i < n) out[i] = sqrtf(in[i]);
-}
-
-int launch_rope_table(float* cos_t, float* sin_t, int max_seq, int d, float theta, cudaStream_t s) {
-    size_t n = (size_t)max_seq * (d / 2);
-    k_rope_table<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(cos_t, sin_t, max_seq, d / 2, theta);
-    CASS_LAUNCH_CHECK();
-    return CASS_OK;
 }
 
 int launch_embed(const int32_t* toks, int rps, int seq_stride, const uint16_t* embed, uint16_t* h, int rows, int hidden, cudaStream_t s) {

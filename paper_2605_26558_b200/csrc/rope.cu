@@ -1,0 +1,258 @@
+// Rotary positions of queries and keys in the caller's layout: y = g (cos t, -sin t; sin t, cos t) (a, b) for every pair of a head,
+// t = position * frequency of the pair.
+// Bound: memory (each value read and written once).  A CTA takes the rows whose sines and cosines its threads form in one go, one
+// (row, pair) a thread: the angle in 64 bits, reduced there to a quarter turn, then sincospif of at most 1/4, so that far positions
+// are as exact as near ones and no table bounds the positions.  All heads of the row share them through shared memory; a thread's
+// values travel while they are formed.  16-byte accesses where the layout allows them, else single values.
+#include <cmath>
+#include <cuda_fp16.h>
+
+#include "kernels.cuh"
+
+namespace cass {
+
+// ---- frequencies ----
+
+bool rope_params_ok(const cass_rope_params& p) {
+    if (p.rot_dim < 2 || p.rot_dim % 2 || p.scaling < CASS_ROPE_PLAIN || p.scaling > CASS_ROPE_YARN) return false;
+    if (!(p.theta > 1.0) || !std::isfinite(p.theta) || !(p.gain >= 0.0) || !std::isfinite(p.gain)) return false;
+    if (p.scaling != CASS_ROPE_PLAIN && (!(p.factor > 0.0) || !std::isfinite(p.factor))) return false;
+    if (p.scaling == CASS_ROPE_NTK && p.rot_dim <= 2) return false;
+    if (p.scaling == CASS_ROPE_BANDS || p.scaling == CASS_ROPE_YARN)
+        return p.low > 0.0 && p.high > p.low && std::isfinite(p.high) && p.trained_len > 0.0 && std::isfinite(p.trained_len);
+    return true;
+}
+
+__device__ double rope_frequency(const cass_rope_params& p, int j) {
+    constexpr double kTwoPi = 6.283185307179586476925;
+    const double r = (double)p.rot_dim;
+    const double theta = p.scaling == CASS_ROPE_NTK ? p.theta * pow(p.factor, r / (r - 2.0)) : p.theta;
+    const double f = pow(theta, -2.0 * (double)j / r);
+    if (p.scaling == CASS_ROPE_LINEAR) return f / p.factor;
+    if (p.scaling == CASS_ROPE_BANDS) {
+        const double turns = p.trained_len * f / kTwoPi, m = fmin(fmax((turns - p.low) / (p.high - p.low), 0.0), 1.0);
+        return m * f + (1.0 - m) * f / p.factor;
+    }
+    if (p.scaling == CASS_ROPE_YARN) {
+        const double half = r / (2.0 * log(p.theta));                   // pair that makes u turns: half * ln(trained_len / (2 pi u))
+        const double a = fmax(floor(half * log(p.trained_len / (kTwoPi * p.high))), 0.0);
+        const double b = fmin(ceil(half * log(p.trained_len / (kTwoPi * p.low))), r - 1.0);
+        const double m = fmin(fmax(((double)j - a) / fmax(b - a, 0.001), 0.0), 1.0);
+        return m * f / p.factor + (1.0 - m) * f;
+    }
+    return f;
+}
+
+__device__ double rope_gain(const cass_rope_params& p) {
+    if (p.gain > 0.0) return p.gain;
+    return p.scaling == CASS_ROPE_YARN && p.factor > 1.0 ? 0.1 * log(p.factor) + 1.0 : 1.0;
+}
+
+__global__ void k_rope_freqs(cass_rope_params p, double* __restrict__ freqs) {
+    const int half = p.rot_dim / 2;
+    for (int j = blockIdx.x * blockDim.x + threadIdx.x; j <= half; j += gridDim.x * blockDim.x) freqs[j] = j < half ? rope_frequency(p, j) : rope_gain(p);
+}
+
+// The session's tables: cosines and sines of every position and pair.
+__global__ void k_rope_table(float* __restrict__ cos_t, float* __restrict__ sin_t, int max_seq, cass_rope_params p) {
+    const int half = p.rot_dim / 2;
+    const size_t i = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
+    if (i >= (size_t)max_seq * half) return;
+    const double ang = (double)(int)(i / half) * rope_frequency(p, (int)(i % half)), gain = rope_gain(p);
+    cos_t[i] = (float)(cos(ang) * gain);
+    sin_t[i] = (float)(sin(ang) * gain);
+}
+
+int launch_rope_table(float* cos_t, float* sin_t, int max_seq, const cass_rope_params& p, cudaStream_t s) {
+    const size_t n = (size_t)max_seq * (p.rot_dim / 2);
+    k_rope_table<<<(unsigned)((n + 255) / 256), 256, 0, s>>>(cos_t, sin_t, max_seq, p);
+    CASS_LAUNCH_CHECK();
+    return CASS_OK;
+}
+
+// ---- rotation ----
+
+constexpr int kRopeThreads = 256;
+constexpr int kRopeUnroll = 4;             // (row, head, slot) items of a thread under way
+
+// cos and sin of position * frequency.
+__device__ __forceinline__ float2 rope_turn(int pos, double f) {
+    double h = (double)pos * f * 0.318309886183790671538;               // half turns
+    h -= 2.0 * rint(0.5 * h);                                           // -1 .. 1
+    const double q = rint(2.0 * h);                                     // quarter turns
+    float s, c;
+    sincospif((float)(h - 0.5 * q), &s, &c);
+    const int n = (int)q & 3;
+    const float cc = (n & 1) ? s : c, ss = (n & 1) ? c : s;
+    return make_float2(n == 1 || n == 2 ? -cc : cc, n >= 2 ? -ss : ss);
+}
+
+template <class T> struct RopeType;
+template <> struct RopeType<__nv_bfloat16> {
+    static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+};
+template <> struct RopeType<__half> {
+    static __device__ __forceinline__ float get(__half v) { return __half2float(v); }
+    static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
+};
+template <> struct RopeType<float> {
+    static __device__ __forceinline__ float get(float v) { return v; }
+    static __device__ __forceinline__ float put(float v) { return v; }
+};
+
+template <class T, int V> struct alignas(sizeof(T) * V) RopeVec { T v[V]; };
+
+struct RopeArgs {
+    cass_rope_geom g;
+    int rows, per_cta;                     // rows; rows a CTA takes
+    int slots, rot_slots;                  // 2 V values each: all of a head's, and those of its pairs (the rest is copied)
+    int transpose;
+    uint32_t head_magic;                   // u / (query and key heads) = high half of u x magic, for u < per_cta x heads
+};
+
+// A slot is V pairs, 2 V values: two vectors half a rotation apart, or side by side where pairs are interleaved or copied.
+template <class T, int V>
+__global__ void __launch_bounds__(kRopeThreads) k_rope(RopeArgs a, const double* __restrict__ freqs, const int32_t* __restrict__ positions,
+                                                       const T* q, const T* k, T* q_out, T* k_out) {
+    extern __shared__ float2 s_turn[];                                  // [per_cta][rot_dim / 2]
+    using Vec = RopeVec<T, V>;
+    const int tid = threadIdx.x, half = a.g.rot_dim / 2, heads = a.g.n_q_heads + a.g.n_k_heads;
+    const int row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
+    const int lanes = min(a.slots, kRopeThreads), ny = kRopeThreads / lanes;     // slots side by side, (row, head)s at a time
+    const int y = tid / lanes, x0 = tid - y * lanes, total = rows * heads;
+    pdl_wait();
+    pdl_early<0>();
+    const double gain = freqs[half];
+    for (int i = tid; i < rows * half; i += kRopeThreads) {
+        const int r = i / half, j = i - r * half;
+        float2 t = rope_turn(positions ? positions[row0 + r] : row0 + r, freqs[j]);
+        if (a.transpose) t.y = -t.y;
+        s_turn[i] = make_float2(t.x * (float)gain, t.y * (float)gain);
+    }
+    __syncthreads();
+    if (y >= ny) return;
+    for (int x = x0; x < a.slots; x += lanes) {
+        const bool turns = x < a.rot_slots;
+        // where the slot's two vectors begin within a head
+        const int lo = turns && !a.g.interleaved ? x * V : x * 2 * V, hi = turns && !a.g.interleaved ? half + x * V : lo + V;
+        const bool has_lo = V > 1 || lo < a.g.head_dim, has_hi = V > 1 || hi < a.g.head_dim;        // single values: an odd head's last
+        for (int u0 = y; u0 < total; u0 += ny * kRopeUnroll) {
+            Vec vl[kRopeUnroll], vh[kRopeUnroll];
+            T* to[kRopeUnroll];
+            int row[kRopeUnroll];
+#pragma unroll
+            for (int i = 0; i < kRopeUnroll; ++i) {
+                const int u = u0 + i * ny;
+                to[i] = nullptr;
+                if (u >= total) continue;
+                row[i] = heads == 1 ? u : (int)__umulhi((uint32_t)u, a.head_magic);
+                const int head = u - row[i] * heads, kh = head - a.g.n_q_heads;
+                const int64_t r = row0 + row[i];
+                const T* from = kh < 0 ? q + r * a.g.q_row + head * a.g.q_head : k + r * a.g.k_row + kh * a.g.k_head;
+                to[i] = kh < 0 ? q_out + r * a.g.q_out_row + head * a.g.q_out_head : k_out + r * a.g.k_out_row + kh * a.g.k_out_head;
+                if (has_lo) vl[i] = *reinterpret_cast<const Vec*>(from + lo);
+                if (has_hi) vh[i] = *reinterpret_cast<const Vec*>(from + hi);
+            }
+#pragma unroll
+            for (int i = 0; i < kRopeUnroll; ++i) {
+                if (!to[i]) continue;
+                if (turns) {
+                    const float2* t = s_turn + row[i] * half + x * V;
+                    T v[2 * V];
+#pragma unroll
+                    for (int j = 0; j < V; ++j) { v[j] = vl[i].v[j]; v[V + j] = vh[i].v[j]; }
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        const int ia = a.g.interleaved ? 2 * j : j, ib = a.g.interleaved ? 2 * j + 1 : V + j;
+                        const float2 y2 = rope_pair(RopeType<T>::get(v[ia]), RopeType<T>::get(v[ib]), t[j].x, t[j].y);
+                        v[ia] = RopeType<T>::put(y2.x);
+                        v[ib] = RopeType<T>::put(y2.y);
+                    }
+#pragma unroll
+                    for (int j = 0; j < V; ++j) { vl[i].v[j] = v[j]; vh[i].v[j] = v[V + j]; }
+                }
+                if (has_lo) *reinterpret_cast<Vec*>(to[i] + lo) = vl[i];
+                if (has_hi) *reinterpret_cast<Vec*>(to[i] + hi) = vh[i];
+            }
+        }
+    }
+}
+
+// Cells of `inner` values at row_stride * row + head_stride * head that do not overlap.
+static bool cells_apart(int64_t rows, int64_t heads, int64_t row_stride, int64_t head_stride, int64_t inner) {
+    if (row_stride < 0 || head_stride < 0) return false;
+    if (rows <= 1) return heads <= 1 || head_stride >= inner;
+    if (heads <= 1) return row_stride >= inner;
+    if (head_stride >= inner && row_stride >= (heads - 1) * head_stride + inner) return true;
+    return row_stride >= inner && head_stride >= (rows - 1) * row_stride + inner;
+}
+
+template <class T>
+static int run_rope(const cass_rope_geom& g, const double* freqs, const int32_t* positions, int rows, const void* q, const void* k, void* q_out,
+                    void* k_out, int transpose, cudaStream_t s) {
+    constexpr int V = 16 / sizeof(T);
+    RopeArgs a{};
+    a.g = g;
+    a.rows = rows;
+    a.transpose = transpose;
+    const int half = g.rot_dim / 2, heads = g.n_q_heads + g.n_k_heads;
+    const bool in_place = (!q || q == q_out) && (!k || k == k_out);
+    const int copied = in_place ? 0 : g.head_dim - g.rot_dim;            // values behind the pairs that have to move
+    int64_t strides = 0;
+    if (q) strides |= g.q_row | g.q_head | g.q_out_row | g.q_out_head;
+    if (k) strides |= g.k_row | g.k_head | g.k_out_row | g.k_out_head;
+    const uintptr_t at = (uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out;
+    const bool wide = half % V == 0 && copied % (2 * V) == 0 && strides % V == 0 && at % 16 == 0;
+    const int v = wide ? V : 1;
+    a.rot_slots = half / v;
+    a.slots = a.rot_slots + ceil_div(copied, 2 * v);
+    a.per_cta = half >= kRopeThreads ? 1 : kRopeThreads / half;
+    if (a.per_cta > ceil_div(rows, kSms)) a.per_cta = ceil_div(rows, kSms);      // few rows: all SMs before full CTAs
+    while (a.per_cta > 1 && (int64_t)a.per_cta * heads > 4096) a.per_cta /= 2;
+    if ((int64_t)a.per_cta * heads > 65535) return CASS_ERR_UNSUPPORTED;
+    a.head_magic = heads == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)heads + 1u;         // u x heads < 2^32
+    const size_t smem = (size_t)a.per_cta * half * sizeof(float2);
+    const dim3 grid(ceil_div(rows, a.per_cta));
+    if (wide)
+        CASS_PDL_LAUNCH((k_rope<T, V>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
+    else
+        CASS_PDL_LAUNCH((k_rope<T, 1>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
+    return CASS_OK;
+}
+
+}  // namespace cass
+
+using namespace cass;
+
+extern "C" int cass_rope_freqs(const cass_rope_params* params, double* freqs, void* stream_) {
+    if (!params || !freqs || ((uintptr_t)freqs & 7) || !rope_params_ok(*params)) return CASS_ERR_INVALID_ARG;
+    k_rope_freqs<<<1, 128, 0, (cudaStream_t)stream_>>>(*params, freqs);
+    CASS_LAUNCH_CHECK();
+    return CASS_OK;
+}
+
+extern "C" int cass_rope(const cass_rope_geom* geom, const double* freqs, const int32_t* positions, int rows, const void* q, const void* k,
+                         void* q_out, void* k_out, int transpose, void* stream_) {
+    if (!geom || !freqs || ((uintptr_t)freqs & 7) || rows < 0) return CASS_ERR_INVALID_ARG;
+    cass_rope_geom g = *geom;
+    if (g.dtype != CASS_BF16 && g.dtype != CASS_F16 && g.dtype != CASS_F32) return CASS_ERR_INVALID_ARG;
+    if (g.rot_dim < 2 || g.rot_dim % 2 || g.head_dim < g.rot_dim || g.n_q_heads < 0 || g.n_k_heads < 0) return CASS_ERR_INVALID_ARG;
+    if (g.rot_dim > 4096) return CASS_ERR_UNSUPPORTED;                   // one row's sines and cosines in shared memory
+    if ((g.n_q_heads > 0) != (q != nullptr) || (g.n_k_heads > 0) != (k != nullptr) || (!q && !k)) return CASS_ERR_INVALID_ARG;
+    if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return CASS_ERR_INVALID_ARG;
+    const int64_t heads = (int64_t)g.n_q_heads + g.n_k_heads;
+    if (heads > 65535 || heads * rows > 0x7FFFFFFFll) return CASS_ERR_UNSUPPORTED;
+    const uintptr_t size = g.dtype == CASS_F32 ? 4 : 2;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out) % size || ((uintptr_t)positions & 3)) return CASS_ERR_INVALID_ARG;
+    if (q && (g.q_row < 0 || g.q_head < 0 || !cells_apart(rows, g.n_q_heads, g.q_out_row, g.q_out_head, g.head_dim))) return CASS_ERR_INVALID_ARG;
+    if (k && (g.k_row < 0 || g.k_head < 0 || !cells_apart(rows, g.n_k_heads, g.k_out_row, g.k_out_head, g.head_dim))) return CASS_ERR_INVALID_ARG;
+    // the same place in another layout would be read after it was written
+    if (q && q == q_out && ((rows > 1 && g.q_row != g.q_out_row) || (g.n_q_heads > 1 && g.q_head != g.q_out_head))) return CASS_ERR_INVALID_ARG;
+    if (k && k == k_out && ((rows > 1 && g.k_row != g.k_out_row) || (g.n_k_heads > 1 && g.k_head != g.k_out_head))) return CASS_ERR_INVALID_ARG;
+    if (rows == 0) return CASS_OK;
+    cudaStream_t s = (cudaStream_t)stream_;
+    if (g.dtype == CASS_BF16) return run_rope<__nv_bfloat16>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
+    if (g.dtype == CASS_F16) return run_rope<__half>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
+    return run_rope<float>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
+}

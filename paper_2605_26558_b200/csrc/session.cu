@@ -263,7 +263,9 @@ extern "C" int cass_session_init(void* mem, size_t bytes, const cass_model_desc*
     s->embed = weights->embed; s->lm_head = weights->lm_head; s->norm_final = weights->norm_final;
     if (cudaMemsetAsync(mem, 0, need, stream) != cudaSuccess) { delete s; return CASS_ERR_CUDA; }
     if (cudaMemcpyAsync(&s->st->max_seq, &s->d.max_seq, 4, cudaMemcpyHostToDevice, stream) != cudaSuccess) { delete s; return CASS_ERR_CUDA; }
-    rc = launch_rope_table(s->cos_t, s->sin_t, desc->max_seq, desc->head_dim, desc->rope_theta, stream);
+    cass_rope_params rope{};
+    rope.rot_dim = desc->head_dim; rope.scaling = CASS_ROPE_PLAIN; rope.theta = desc->rope_theta;
+    rc = launch_rope_table(s->cos_t, s->sin_t, desc->max_seq, rope, stream);
     if (!rc && blobs) rc = read_blob_infos(s, blobs, stream);
     if (!rc && cudaStreamSynchronize(stream) != cudaSuccess) rc = CASS_ERR_CUDA;
     if (rc) { delete s; return rc; }
@@ -274,6 +276,13 @@ extern "C" int cass_session_init(void* mem, size_t bytes, const cass_model_desc*
 extern "C" int cass_session_set_blobs(void* session, const cass_model_blobs* blobs, void* stream_) {
     if (!session || !blobs || !blobs->h_layers) return CASS_ERR_INVALID_ARG;
     return read_blob_infos((Session*)session, blobs, (cudaStream_t)stream_);
+}
+
+extern "C" int cass_session_set_rope(void* session, const cass_rope_params* params, void* stream_) {
+    if (!session || !params || !rope_params_ok(*params)) return CASS_ERR_INVALID_ARG;
+    Session* s = (Session*)session;
+    if (params->rot_dim != s->d.head_dim) return CASS_ERR_UNSUPPORTED;
+    return launch_rope_table(s->cos_t, s->sin_t, s->d.max_seq, *params, (cudaStream_t)stream_);
 }
 
 extern "C" int cass_session_destroy(void* session) {
