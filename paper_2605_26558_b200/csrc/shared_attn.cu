@@ -471,11 +471,18 @@ __device__ SaParts shared_parts(const SharedAttn& a, int seg_pairs, int b, int h
         r.pre0 = (int64_t)(w0 + s) * a.pairs + all % seg_pairs;
         r.pre_step = a.pairs;
         r.n_pre = w1 - w0 + 1;
-    } else if (a.pre_splits) {
+    } else if (a.prefix) {
+        const int cta = all / (2 * kStTile);
         r.pre_tc = true;
-        r.pre0 = (int64_t)head * a.pre_pairs + all;
-        r.pre_step = (int64_t)a.n_kv * a.pre_pairs;
-        r.n_pre = a.pre_splits;
+        if (cta < a.pre_n2) {
+            r.pre0 = ((int64_t)head * a.pre_n2 + cta) * 2 * kStTile + all % (2 * kStTile);
+            r.pre_step = (int64_t)a.n_kv * a.pre_n2 * 2 * kStTile;
+            r.n_pre = a.pre_s2;
+        } else {
+            r.pre0 = a.pre_at1 + (int64_t)head * kStTile + all % (2 * kStTile);
+            r.pre_step = (int64_t)a.n_kv * kStTile;
+            r.n_pre = 2 * a.pre_s1;
+        }
     }
     const int tiles = ceil_div(max(n, 0), kSaTok);
     if (tiles) {
@@ -615,6 +622,8 @@ struct SaPlan {
     size_t at_o, at_m, at_l, at_scores, at_pre_o, at_pre_m, at_pre_l, bytes;
 };
 
+constexpr int kSaStreamPairs = 64;                       // pairs behind a prefix up to which it is streamed
+
 static bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
 
 static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool with_weights, SaPlan* plan) {
@@ -624,6 +633,8 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     const int64_t in[] = {t->q_seq, t->q_row, t->q_head, t->out_seq, t->out_row, t->out_head, t->prefix_pos_stride, t->prefix_head_stride};
     for (int64_t s : in)
         if (s < 0 || s % 8 || s > ((int64_t)1 << 46)) return CASS_ERR_INVALID_ARG;
+    if ((t->prefix_len > 1 && t->prefix_pos_stride < c->head_dim) || (t->prefix_len && c->n_kv_heads > 1 && t->prefix_head_stride < c->head_dim))
+        return CASS_ERR_INVALID_ARG;
     // the output's heads lie apart, as rows of a cache do: (sequence, row, head) by its strides
     cass_cache_geom o = *c;
     o.n_kv_heads = t->n_q_heads; o.capacity = t->rows; o.seq_stride = t->out_seq; o.pos_stride = t->out_row; o.head_stride = t->out_head;
@@ -640,7 +651,7 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     a.c_seq = c->seq_stride; a.c_pos = c->pos_stride; a.c_head = c->head_stride;
     a.scale_log2 = (t->scale > 0.f ? t->scale : 1.0f / sqrtf((float)a.d)) * 1.44269504088896341f;
     const int P = a.rows * group, all = a.n_seq * P;     // pairs of a sequence, of all
-    plan->tc = false;
+    plan->tc = a.prefix && all > kSaStreamPairs && shared_tc_usable(a);
     const int most = a.prefix && !plan->tc ? (all > P ? all : P) : P;
     plan->mt = a.d > 128 || most <= 16 ? 1 : most <= 32 ? 2 : 4;
     const int seg = 16 * plan->mt;
@@ -655,6 +666,10 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     plan->at_o = take(slots * a.pairs * a.d * 4);
     plan->at_m = take(slots * a.pairs * 4);
     plan->at_l = take(slots * a.pairs * 4);
+    const size_t pre = plan->tc ? (size_t)shared_tc_plan(a) : 0;
+    plan->at_pre_o = take(pre * a.d * 4);
+    plan->at_pre_m = take(pre * 4);
+    plan->at_pre_l = take(pre * 4);
     plan->at_scores = take(with_weights ? (size_t)a.n_seq * a.n_q * a.rows * a.capacity * 4 : 0);
     plan->bytes = off < 256 ? 256 : off;
     return CASS_OK;
@@ -681,7 +696,9 @@ static int run_stream_d(const SharedAttn& a, int mt, cudaStream_t s) {
 template <int DT>
 static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float* weight_in, float* weight_out, int32_t* d_status, cudaStream_t s) {
     const SharedAttn& a = plan.a;
-    int rc = CASS_ERR_UNSUPPORTED;
+    int rc = plan.tc ? launch_shared_prefix_tc(a, DT, d_status, s) : CASS_OK;
+    if (rc) return rc;
+    rc = CASS_ERR_UNSUPPORTED;
     switch (a.d) {
         case 32: rc = run_stream_d<DT, 32>(a, plan.mt, s); break;
         case 64: rc = run_stream_d<DT, 64>(a, plan.mt, s); break;
@@ -728,6 +745,7 @@ extern "C" int cass_shared_prefix_attention(const cass_cache_geom* cache, const 
     a.q = (const uint16_t*)q; a.kp = (const uint16_t*)k_prefix; a.vp = (const uint16_t*)v_prefix;
     a.kc = (const uint16_t*)k_cache; a.vc = (const uint16_t*)v_cache; a.lens = a.capacity ? lens : nullptr;
     a.part_o = (float*)(mem + plan.at_o); a.part_m = (float*)(mem + plan.at_m); a.part_l = (float*)(mem + plan.at_l);
+    a.pre_o = (float*)(mem + plan.at_pre_o); a.pre_m = (float*)(mem + plan.at_pre_m); a.pre_l = (float*)(mem + plan.at_pre_l);
     a.scores = weight_out ? (float*)(mem + plan.at_scores) : nullptr;
     if (cache->dtype == CASS_BF16) return run_shared<CASS_BF16>(plan, (uint16_t*)out, lse, weight_in, weight_out, d_status, (cudaStream_t)stream_);
     return run_shared<CASS_F16>(plan, (uint16_t*)out, lse, weight_in, weight_out, d_status, (cudaStream_t)stream_);

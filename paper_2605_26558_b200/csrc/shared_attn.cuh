@@ -20,10 +20,18 @@ struct SharedAttn {
     // the streaming kernel's work
     int ctas, pairs;                                     // CTAs; pairs of a segment
     int p_groups, c_groups;                              // segments of pairs of the prefix (0: not this kernel's) and of a sequence
-    // the prefix by the tensor-core kernel: parts [split][head][pair of all sequences]
+    // The prefix by the tensor-core kernel: the pairs of all sequences in tiles of 128.  Two tiles a CTA, `pre_n2` CTAs a head, its positions over
+    // `pre_s2` CTAs: parts [split][head][CTA][256].  What is left over, one tile, over `pre_s1` (0: nothing is left): parts
+    // [2 split + warpgroup][head][128], pre_at1 pairs further.
     float *pre_o, *pre_m, *pre_l;
-    int pre_splits, pre_pairs;
+    int pre_n2, pre_s2, pre_s1;
+    int64_t pre_at1;
 };
+constexpr int kStTile = 128;                             // pairs and positions of a tile of that kernel
+
+// Whether the tensor-core kernel can take this prefix, and over how many CTAs; the number of pairs that its parts hold.
+bool shared_tc_usable(const SharedAttn& a);
+int64_t shared_tc_plan(SharedAttn& a);
 
 // Positions of sequence b's cache; -1: the sequence is not there.
 __device__ __forceinline__ int shared_len(const SharedAttn& a, int b) {
