@@ -448,7 +448,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::warps * 32) k_shared_stream(Sh
 
 // ---- joining the parts ----
 constexpr int kSmThreads = 128, kSmWarps = kSmThreads / 32;
-constexpr int kSmMaxParts = 1024;
+constexpr int kSmMaxParts = 4 * kSms;                // of a pair: at most every CTA's of either kernel, and two a CTA of the tensor-core kernel's
 constexpr int kSmPos = 4 * kSmThreads;                   // positions of a weights block
 
 // Where the parts of (sequence b, head, pair p of the sequence) lie: those of the prefix, then those of its cache, in order.
@@ -496,72 +496,83 @@ __device__ SaParts shared_parts(const SharedAttn& a, int seg_pairs, int b, int h
     return r;
 }
 
-// grid: a block for every (sequence, row, query head), then (with weights) one for every 512 positions of every (sequence, KV head)
-template <int DT>
-__global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int seg_pairs, int pos_blocks, uint16_t* __restrict__ out,
+// grid: blocks of the (sequence, row, query head)s, WARPS warps each, then (with weights) one for every 512 positions of every (sequence, KV
+// head).  A warp a pair where there are many pairs, four where there are few with many parts.
+template <int DT, int WARPS>
+__global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int seg_pairs, int pair_blocks, int pos_blocks, uint16_t* __restrict__ out,
                                                              float* __restrict__ lse, const float* weight_in, float* weight_out,
                                                              int32_t* __restrict__ d_status) {
     using T = SaType<DT>;
-    __shared__ float s_w[kSmMaxParts];
-    __shared__ float s_o[kSmWarps][256];
-    __shared__ int s_before[kSmWarps], s_all[kSmWarps];
+    __shared__ float s_w[kSmWarps][kSmMaxParts];
+    __shared__ __align__(16) float s_o[kSmWarps][256];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_wait();
     pdl_early<3>();
-    const int n_pairs = a.n_seq * a.rows * a.n_q, P = a.rows * a.group;
-    const bool weights = (int)blockIdx.x >= n_pairs;
-    int b, head, p, chunk = 0;
+    const int P = a.rows * a.group;
+    const bool weights = (int)blockIdx.x >= pair_blocks;
+    int b, head, p = 0, r = 0, hq = 0, chunk = 0;
     if (weights) {
-        int i = blockIdx.x - n_pairs;
+        int i = blockIdx.x - pair_blocks;
         chunk = i % pos_blocks; i /= pos_blocks;
-        head = i % a.n_kv; b = i / a.n_kv; p = 0;
+        head = i % a.n_kv; b = i / a.n_kv;
     } else {
-        const int hq = blockIdx.x % a.n_q, r = blockIdx.x / a.n_q % a.rows;
-        b = blockIdx.x / a.n_q / a.rows; head = hq / a.group; p = r * a.group + hq % a.group;
+        const int i = blockIdx.x * (kSmWarps / WARPS) + warp / WARPS;
+        hq = i % a.n_q; r = i / a.n_q % a.rows; b = i / a.n_q / a.rows;
+        if (b >= a.n_seq) return;
+        head = hq / a.group; p = r * a.group + hq % a.group;
     }
     const int n = shared_len(a, b);
     if (n < 0) return;                                   // the sequence is not there
-    if (!weights && p == 0 && head == 0 && tid == 0 && a.lens && a.lens[b] > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
     int before = 0, tiles = 0;
-    for (int i = tid; i < a.n_seq; i += kSmThreads) {
+    for (int i = lane; i < a.n_seq; i += 32) {
         const int t = ceil_div(max(shared_len(a, i), 0), kSaTok);
         tiles += t;
         before += i < b ? t : 0;
     }
     before = __reduce_add_sync(0xffffffffu, before);
     tiles = __reduce_add_sync(0xffffffffu, tiles);
-    if (lane == 0) { s_before[warp] = before; s_all[warp] = tiles; }
-    __syncthreads();
-    before = tiles = 0;
-#pragma unroll
-    for (int w = 0; w < kSmWarps; ++w) { before += s_before[w]; tiles += s_all[w]; }
 
-    auto m_of = [&](const SaParts& s, int i) {
-        return i < s.n_pre ? (s.pre_tc ? a.pre_m : a.part_m)[s.pre0 + i * s.pre_step] : a.part_m[s.own0 + (int64_t)(i - s.n_pre) * s.own_step];
-    };
-    auto l_of = [&](const SaParts& s, int i) {
-        return i < s.n_pre ? (s.pre_tc ? a.pre_l : a.part_l)[s.pre0 + i * s.pre_step] : a.part_l[s.own0 + (int64_t)(i - s.n_pre) * s.own_step];
-    };
-    // a warp's sum over all parts of 2^(m - M) l, and M
-    auto sums = [&](const SaParts& s, float& M, float& L) {
-        M = -INFINITY;
-        for (int i = lane; i < s.count(); i += 32) M = fmaxf(M, m_of(s, i));
+    // maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M)
+    auto sums = [&](const SaParts& s, float* w, float& M, float& L) {
+        const float *pm = s.pre_tc ? a.pre_m : a.part_m, *pl = s.pre_tc ? a.pre_l : a.part_l;
+        const int count = s.count();
+        float m0 = -INFINITY, l0 = 0.f;                  // of the first 32, one round trip
+        auto load = [&](int i, float& m, float& l) {
+            if (i < s.n_pre) { m = pm[s.pre0 + i * s.pre_step]; l = pl[s.pre0 + i * s.pre_step]; }
+            else { const int64_t at = s.own0 + (int64_t)(i - s.n_pre) * s.own_step; m = a.part_m[at]; l = a.part_l[at]; }
+        };
+        if (lane < count) load(lane, m0, l0);
+        M = m0;
+        for (int i = lane + 32; i < count; i += 32) {
+            float m, l;
+            load(i, m, l);
+            M = fmaxf(M, m);
+        }
         M = warp_max(M);
         const float base = M == -INFINITY ? 0.f : M;
-        L = 0.f;
-        for (int i = lane; i < s.count(); i += 32) L += exp2_fast(m_of(s, i) - base) * l_of(s, i);
+        const float f0 = exp2_fast(m0 - base);
+        L = f0 * l0;
+        if (w && lane < count) w[lane] = f0;
+        for (int i = lane + 32; i < count; i += 32) {
+            float m, l;
+            load(i, m, l);
+            const float f = exp2_fast(m - base);
+            L += f * l;
+            if (w) w[i] = f;
+        }
         L = warp_sum(L);
+        __syncwarp();
     };
     if (weights) {
         const int pos0 = chunk * kSmPos;
         const float* in = weight_in ? weight_in + ((int64_t)b * a.n_kv + head) * a.capacity : nullptr;
         float* to = weight_out + ((int64_t)b * a.n_kv + head) * a.capacity;
+        float* s_lse = &s_w[0][0];
         if (pos0 < n) {
             for (int q = warp; q < P; q += kSmWarps) {
-                const SaParts s = shared_parts(a, seg_pairs, b, head, q, before, tiles, n);
                 float M, L;
-                sums(s, M, L);
-                if (lane == 0) s_w[q] = M + log2f(L);
+                sums(shared_parts(a, seg_pairs, b, head, q, before, tiles, n), nullptr, M, L);
+                if (lane == 0) s_lse[q] = M + log2f(L);
             }
             __syncthreads();
         }
@@ -571,46 +582,53 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
             const int pos = pos0 + i * kSmThreads + tid;
             if (pos >= a.capacity) break;
             float sum = 0.f;
-            for (int r = 0; r < a.rows; ++r) {
-                if (pos >= n - (a.rows - 1 - r)) continue;
-                for (int g = 0; g < a.group; ++g) sum += exp2_fast(from[(int64_t)(r * a.group + g) * a.capacity + pos] - s_w[r * a.group + g]);
+            for (int q = 0; q < a.rows; ++q) {
+                if (pos >= n - (a.rows - 1 - q)) continue;
+                for (int g = 0; g < a.group; ++g) sum += exp2_fast(from[(int64_t)(q * a.group + g) * a.capacity + pos] - s_lse[q * a.group + g]);
             }
             if (pos < n || in != to) to[pos] = (in ? in[pos] : 0.f) + sum;
         }
         return;
     }
-    const int r = p / a.group, hq = head * a.group + p % a.group;
+    if (p == 0 && head == 0 && warp % WARPS == 0 && lane == 0 && a.lens && a.lens[b] > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
     const SaParts s = shared_parts(a, seg_pairs, b, head, p, before, tiles, n);
     const int parts = s.count();
-    float M, L;
-    sums(s, M, L);                                       // every warp the same
-    const float base = M == -INFINITY ? 0.f : M;
-    for (int i = tid; i < parts; i += kSmThreads) s_w[i] = exp2_fast(m_of(s, i) - base);
-    __syncthreads();
-    for (int c = lane * 4; c < a.d; c += 128) {
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-        for (int i = warp; i < parts; i += kSmWarps) {
-            const float* from = i < s.n_pre ? (s.pre_tc ? a.pre_o : a.part_o) + (s.pre0 + i * s.pre_step) * a.d
-                                            : a.part_o + (s.own0 + (int64_t)(i - s.n_pre) * s.own_step) * a.d;
-            const float4 x = *reinterpret_cast<const float4*>(from + c);
-            const float w = s_w[i];
-            sum.x = fmaf(w, x.x, sum.x); sum.y = fmaf(w, x.y, sum.y); sum.z = fmaf(w, x.z, sum.z); sum.w = fmaf(w, x.w, sum.w);
-        }
-        *reinterpret_cast<float4*>(&s_o[warp][c]) = sum;
-    }
-    __syncthreads();
+    float M, L, *w = s_w[warp];
+    sums(s, w, M, L);                                    // each of the pair's warps for itself
+    const float* po = s.pre_tc ? a.pre_o : a.part_o;
     const bool sees = a.prefix > 0 || n - (a.rows - 1 - r) > 0;
     uint16_t* to = out + (int64_t)b * a.out_seq + (int64_t)r * a.out_row + (int64_t)hq * a.out_head;
-    for (int c = tid * 2; c < a.d; c += kSmThreads * 2) {
-        float x = 0.f, y = 0.f;
-#pragma unroll
-        for (int w = 0; w < kSmWarps; ++w) { x += s_o[w][c]; y += s_o[w][c + 1]; }
-        x = sees ? x / L : 0.f;
-        y = sees ? y / L : 0.f;
-        *reinterpret_cast<uint32_t*>(to + c) = T::put(x) | ((uint32_t)T::put(y) << 16);
+    auto put = [&](int c, float4 x) {
+        const uint32_t lo = T::put(sees ? x.x / L : 0.f) | ((uint32_t)T::put(sees ? x.y / L : 0.f) << 16);
+        const uint32_t hi = T::put(sees ? x.z / L : 0.f) | ((uint32_t)T::put(sees ? x.w / L : 0.f) << 16);
+        *reinterpret_cast<uint2*>(to + c) = make_uint2(lo, hi);
+    };
+    for (int c = lane * 4; c < a.d; c += 128) {
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+        for (int i = warp % WARPS; i < parts; i += WARPS) {
+            const float* from = i < s.n_pre ? po + (s.pre0 + i * s.pre_step) * a.d : a.part_o + (s.own0 + (int64_t)(i - s.n_pre) * s.own_step) * a.d;
+            const float4 x = *reinterpret_cast<const float4*>(from + c);
+            const float f = w[i];
+            sum.x = fmaf(f, x.x, sum.x); sum.y = fmaf(f, x.y, sum.y); sum.z = fmaf(f, x.z, sum.z); sum.w = fmaf(f, x.w, sum.w);
+        }
+        if (WARPS == 1) put(c, sum);
+        else *reinterpret_cast<float4*>(&s_o[warp][c]) = sum;
     }
-    if (lse && tid == 0) lse[((int64_t)b * a.rows + r) * a.n_q + hq] = sees ? (M + log2f(L)) * 0.693147180559945309f : -INFINITY;
+    if (WARPS > 1) {
+        __syncthreads();
+        if (warp == 0)
+            for (int c = lane * 4; c < a.d; c += 128) {
+                float4 x = *reinterpret_cast<const float4*>(&s_o[0][c]);
+#pragma unroll
+                for (int i = 1; i < WARPS; ++i) {
+                    const float4 y = *reinterpret_cast<const float4*>(&s_o[i][c]);
+                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
+                }
+                put(c, x);
+            }
+    }
+    if (lse && warp % WARPS == 0 && lane == 0) lse[((int64_t)b * a.rows + r) * a.n_q + hq] = sees ? (M + log2f(L)) * 0.693147180559945309f : -INFINITY;
 }
 
 // ---- host ----
@@ -622,6 +640,7 @@ struct SaPlan {
     size_t at_o, at_m, at_l, at_scores, at_pre_o, at_pre_m, at_pre_l, bytes;
 };
 
+constexpr int kSmManyPairs = 4 * kSms;                   // joined by a warp each
 constexpr int kSaStreamPairs = 64;                       // pairs behind a prefix up to which it is streamed
 
 static bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
@@ -709,10 +728,16 @@ static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float
     }
     if (rc) return rc;
     const int pos_blocks = weight_out ? ceil_div(a.capacity, kSmPos) : 0;
-    const int64_t blocks = (int64_t)a.n_seq * a.rows * a.n_q + (int64_t)a.n_seq * a.n_kv * pos_blocks;
+    const int64_t pairs = (int64_t)a.n_seq * a.rows * a.n_q;
+    const bool many = pairs >= kSmManyPairs;
+    const int64_t pair_blocks = many ? (pairs + kSmWarps - 1) / kSmWarps : pairs, blocks = pair_blocks + (int64_t)a.n_seq * a.n_kv * pos_blocks;
     if (blocks > 0x7FFFFFFF) return CASS_ERR_UNSUPPORTED;
-    CASS_PDL_LAUNCH(k_shared_merge<DT>, dim3((unsigned)blocks), dim3(kSmThreads), 0, s, a, 16 * plan.mt, pos_blocks, out, lse, weight_in, weight_out,
-                    d_status);
+    if (many)
+        CASS_PDL_LAUNCH((k_shared_merge<DT, 1>), dim3((unsigned)blocks), dim3(kSmThreads), 0, s, a, 16 * plan.mt, (int)pair_blocks, pos_blocks, out, lse,
+                        weight_in, weight_out, d_status);
+    else
+        CASS_PDL_LAUNCH((k_shared_merge<DT, kSmWarps>), dim3((unsigned)blocks), dim3(kSmThreads), 0, s, a, 16 * plan.mt, (int)pair_blocks, pos_blocks, out,
+                        lse, weight_in, weight_out, d_status);
     return CASS_OK;
 }
 

@@ -25,6 +25,8 @@ struct StShape {
     static constexpr int q_tile = kStTile * D * 2;       // Q of 128 pairs; K or V of 128 positions: boxes of 128 x 64, 128-byte swizzle
     static constexpr int slots = D == 128 ? 5 : 8;
     static constexpr int smem = (2 + slots) * q_tile + 256 + 1024;
+    static_assert(slots * q_tile >= 8 * 32 * D * 4, "the outputs pass through the ring");
+    static_assert(smem <= (int)kSmemPerBlock, "shared memory of a CTA");
 };
 
 __device__ __forceinline__ void st_mma_tmem_a(uint32_t tmem_d, uint32_t tmem_a, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
@@ -89,6 +91,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
     uint64_t* full = reinterpret_cast<uint64_t*>(sT + S::slots * kTile);
     uint64_t *empty = full + S::slots, *s_full = empty + S::slots, *p_done = s_full + 2, *o_full = p_done + 2;
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
+    int64_t* s_q = reinterpret_cast<int64_t*>(sT + (S::slots - 1) * kTile);      // where a pair's query lies, -1: there is none; before the slot's first tile
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     // ---- which pairs, which positions ----
     const int ctas2 = a.pre_s2 * a.n_kv * a.pre_n2;
@@ -110,17 +113,44 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     pdl_wait();
+    // K and V tiles in the order of the products that read them; the first ones travel while Q is gathered
+    int it = 0;
+    bool ok = true;
+    const int ahead = two ? 1 : 2;                       // score products before the first output product
+    auto load = [&](int x) {                             // the x-th tile of that order
+        const int lead = min(ahead, n), y = x - lead;    // K 0 .. lead - 1, then V 0, K lead, V 1, ...; V alone at the end
+        const int pairs = n - lead;                      // (V, K) pairs
+        const bool is_v = y >= 0 && (y >= 2 * pairs || y % 2 == 0);
+        const int j = y < 0 ? x : y >= 2 * pairs ? y - pairs : is_v ? y / 2 : y / 2 + lead;
+        const int s = x % S::slots;
+        mbar_expect_tx(&full[s], kTile);
+#pragma unroll
+        for (int b = 0; b < kBoxes; ++b)
+            tma_load_3d(sT + s * kTile + b * kBox, is_v ? &map_v : &map_k, b * 64, head, (j0 + j) * kStTile, &full[s]);
+    };
+    if (tid == 0)
+        for (; it < min(2 * n, S::slots - 1); ++it) load(it);
     if (warp >= 4) {
         // Q: pair p of the tiles = ((sequence x rows + row) x group + head in the group), zeros beyond the last
-        for (int x = tid - 128; x < (two ? 2 : 1) * kStTile * (D / 8); x += kStThreads - 128) {
-            const int p = x / (D / 8), c8 = x % (D / 8), all = first + p;
-            uint4 v = make_uint4(0u, 0u, 0u, 0u);
-            if (all < P) {
-                const int r = all / a.group, g = all - r * a.group, seq = r / a.rows;
-                v = *reinterpret_cast<const uint4*>(a.q + (int64_t)seq * a.q_seq + (int64_t)(r - seq * a.rows) * a.q_row +
-                                                    (int64_t)(head * a.group + g) * a.q_head + c8 * 8);
+        const int x = tid - 128, c8 = x % (D / 8), rows = (two ? 2 : 1) * kStTile;
+        if (x < rows) {
+            const int all = first + x, r = all / a.group, g = all - r * a.group, seq = r / a.rows;
+            s_q[x] = all < P ? (int64_t)seq * a.q_seq + (int64_t)(r - seq * a.rows) * a.q_row + (int64_t)(head * a.group + g) * a.q_head : -1;
+        }
+        asm volatile("bar.sync 1, 256;" ::: "memory");
+        constexpr int kStep = 256 / (D / 8), kUnroll = kStTile / kStep;      // rows at a time, a tile under way
+        for (int p0 = x / (D / 8); p0 < rows; p0 += kStep * kUnroll) {
+            uint4 v[kUnroll];
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int64_t at = s_q[p0 + u * kStep];
+                v[u] = at >= 0 ? *reinterpret_cast<const uint4*>(a.q + at + c8 * 8) : make_uint4(0u, 0u, 0u, 0u);
             }
-            *reinterpret_cast<uint4*>(sQ + (p / kStTile) * kTile + (c8 >> 3) * kBox + (p % kStTile) * 128 + (((c8 ^ p) & 7) << 4)) = v;
+#pragma unroll
+            for (int u = 0; u < kUnroll; ++u) {
+                const int p = p0 + u * kStep;
+                *reinterpret_cast<uint4*>(sQ + (p / kStTile) * kTile + (c8 >> 3) * kBox + (p % kStTile) * 128 + (((c8 ^ p) & 7) << 4)) = v[u];
+            }
         }
         fence_proxy_async();
     }
@@ -131,31 +161,17 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStRegsIssue));
         if (warp == 0) {
-            if (tc_elect()) {
-                // tiles in the order of the products that read them
-                int it = 0;
-                bool ok = true;
-                auto load = [&](const CUtensorMap* map, int j) {
-                    const int s = it % S::slots;
-                    ok = ok && mbar_wait_bounded(&empty[s], ((uint32_t)(it / S::slots) & 1u) ^ 1u);
-                    if (!ok) return;
-                    mbar_expect_tx(&full[s], kTile);
-#pragma unroll
-                    for (int b = 0; b < kBoxes; ++b) tma_load_3d(sT + s * kTile + b * kBox, map, b * 64, head, (j0 + j) * kStTile, &full[s]);
-                    ++it;
-                };
-                const int ahead = two ? 1 : 2;               // score products before the first output product
-                for (int j = 0; j < min(ahead, n); ++j) load(&map_k, j);
-                for (int j = 0; j < n; ++j) {
-                    load(&map_v, j);
-                    if (j + ahead < n) load(&map_k, j + ahead);
+            if (tid == 0) {
+                for (; it < 2 * n; ++it) {
+                    ok = mbar_wait_bounded(&empty[it % S::slots], ((uint32_t)(it / S::slots) & 1u) ^ 1u);
+                    if (!ok) break;
+                    load(it);
                 }
                 if (!ok) atomicCAS(d_status, 0, CASS_ERR_TIMEOUT);
             }
         } else if (warp == 1) {
             if (tc_elect()) {
-                int it = 0;
-                bool ok = true;
+                it = 0;
                 auto tile_in = [&]() -> const uint8_t* {     // the next tile, once it has arrived
                     const int s = it % S::slots;
                     ok = ok && mbar_wait_bounded(&full[s], (uint32_t)(it / S::slots) & 1u);
@@ -239,7 +255,6 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
         const uint32_t lanes = tmem + ((uint32_t)(q * 32) << 16), sc = lanes + kStS + wg * 128, oc = lanes + kStO + wg * 128;
         const int uses = two ? n : (n - wg + 1) / 2;
         float m = -INFINITY, l = 0.f;                    // the base of the numerators; their sum
-        bool ok = true;
         for (int u = 0; u < uses; ++u) {
             const int j = j0 + (two ? u : 2 * u + wg);
             ok = __all_sync(0xffffffffu, ok && mbar_wait_bounded(&s_full[wg], (uint32_t)u & 1u));
@@ -303,17 +318,24 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
             const int64_t at = two ? (((int64_t)split * a.n_kv + head) * a.pre_n2 + cta) * 2 * kStTile + wg * kStTile + row
                                    : a.pre_at1 + ((int64_t)(2 * split + wg) * a.n_kv + head) * kStTile + row;
             if (all < P) { a.pre_m[at] = m; a.pre_l[at] = l; }
+            // through the ring (every product that read it is done), so that a warp's stores are whole rows
+            float4* box = reinterpret_cast<float4*>(sT) + (warp - 4) * 32 * (D / 4);
 #pragma unroll
             for (int c = 0; c < D; c += 32) {
                 float o[32];
                 st_ld32(oc + c, o);
                 st_wait_ld();
-                if (all < P) {
-                    float4* to = reinterpret_cast<float4*>(a.pre_o + at * D + c);
 #pragma unroll
-                    for (int e = 0; e < 32; e += 4)
-                        to[e / 4] = uses ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
-                }
+                for (int e = 0; e < 32; e += 4)
+                    box[lane * (D / 4) + (((c + e) / 4) ^ (lane & 7))] = uses ? make_float4(o[e], o[e + 1], o[e + 2], o[e + 3]) : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+            __syncwarp();
+            float* to = a.pre_o + (at - lane) * D;
+            const int there = min(32, P - (all - lane));
+#pragma unroll 8
+            for (int x = lane; x < there * (D / 4); x += 32) {
+                const int r = x / (D / 4), c = x % (D / 4);
+                reinterpret_cast<float4*>(to)[x] = box[r * (D / 4) + (c ^ (r & 7))];
             }
         } else if (lane == 0) atomicCAS(d_status, 0, CASS_ERR_TIMEOUT);
     }
