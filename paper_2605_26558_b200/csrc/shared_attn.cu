@@ -2,449 +2,10 @@
 // which is read once; every sequence's own cache is read by its own queries.  Both leave partial results (output, maximum, sum) that
 // k_shared_merge joins; the weights that the caches' positions got follow from the scores, once the sums are known.
 //
-// k_shared_stream: tiles of 64 positions, K and V through a ring of asynchronous copies, both products by mma.sync (16 pairs of (row,
-// query head) by 16 positions), softmax in registers with a running maximum.  What is bound by memory runs here: with up to 64 pairs
-// a position's 512 bytes (head size 128) cost less time in the products than on the bus.  The positions of all segments form one list of
-// tiles that the CTAs share evenly, whatever the lengths are; the lengths are read on the device.
-#include <cuda_fp16.h>
-
+// The prefix behind few queries and the caches are shared_stream.cuh's, the prefix behind many is shared_attn_tc.cu's.
 #include "shared_attn.cuh"
 
 namespace cass {
-
-// ---- 16-bit types ----
-template <int DT> struct SaType;
-template <> struct SaType<CASS_BF16> {
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        uint32_t r;
-        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-        return r;
-    }
-    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static constexpr uint32_t kExponent = 0x7F80u;
-    static __device__ __forceinline__ float get(uint32_t v) { return __uint_as_float(v << 16); }
-    static __device__ __forceinline__ uint16_t put(float v) { return float_to_bf16_bits(v); }
-};
-template <> struct SaType<CASS_F16> {
-    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
-        uint32_t r;
-        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-        return r;
-    }
-    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
-    static constexpr uint32_t kExponent = 0x7C00u;
-    static __device__ __forceinline__ float get(uint32_t v) { return __half2float(__ushort_as_half((uint16_t)v)); }
-    static __device__ __forceinline__ uint16_t put(float v) { return __half_as_ushort(__float2half_rn(v)); }
-};
-
-__device__ __forceinline__ void cp16(void* dst, const void* src, bool there) {      // zeros where there is nothing
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_u32(dst)), "l"(src), "r"(there ? 16 : 0) : "memory");
-}
-__device__ __forceinline__ void ldm4(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ void ldm4_t(uint32_t (&r)[4], uint32_t at) {
-    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
-}
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-
-// Byte of 16-byte vector c of a row in shared memory: eight rows' vectors of one column lie in different banks.
-template <int D>
-__device__ __forceinline__ uint32_t sa_at(int row, int c) {
-    return (uint32_t)(row * D * 2 + ((D % 64 == 0 ? c ^ (row & 7) : c ^ ((row >> 1) & 3)) << 4));
-}
-
-template <int D, int MT>
-struct SaShape {
-    static constexpr int warps = MT == 4 ? 8 : 4;
-    static constexpr int groups = warps / MT;            // of positions: a warp takes 64 / groups of a tile's
-    static constexpr int tok = kSaTok / groups;
-    static constexpr int pairs = 16 * MT;
-    static constexpr bool q_regs = D <= 128;             // Q in registers from a segment's first tile on
-    static constexpr int stages = MT == 4 ? 5 : 3;
-    static constexpr int q_bufs = q_regs ? stages - 1 : stages;      // segments that begin in the tiles under way
-    static constexpr int stage_bytes = kSaTok * D * 2 * 2;
-    static constexpr int q_bytes = pairs * D * 2;
-    static constexpr int smem = stages * stage_bytes + q_bufs * q_bytes;
-    static constexpr int per_sm = smem + 1024 + 512 <= 233472 / 2 ? 2 : 1;
-    static_assert((groups - 1) * MT * 64 * D <= stage_bytes, "the joining of a segment's warps fits a stage");
-};
-
-// One segment of the list as a worker sees it.
-struct SaSegment {
-    int index, head, first, seq, n;                      // number; KV head; first pair; sequence (-1: prefix); positions
-    int64_t begin, end;                                  // tiles of the list
-};
-
-template <int DT, int D, int MT>
-__global__ void __launch_bounds__(SaShape<D, MT>::warps * 32) k_shared_stream(SharedAttn a) {
-    using S = SaShape<D, MT>;
-    using T = SaType<DT>;
-    constexpr int kThreads = S::warps * 32;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ int64_t s_scan[S::warps];
-    __shared__ float s_ml[S::groups][S::pairs][2];
-    __shared__ int s_seq, s_before;
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, mt = warp % MT, grp = warp / MT;
-    uint8_t* sQ = smem + S::stages * S::stage_bytes;
-    pdl_wait();
-    pdl_early<2>();
-
-    // ---- the list: tiles of the prefix, then of the sequences ----
-    const int p_tiles = a.p_groups ? ceil_div(a.prefix, kSaTok) : 0, seq_segs = a.c_groups * a.n_kv, p_segs = a.p_groups * a.n_kv;
-    const int64_t p_total = (int64_t)p_tiles * p_segs;
-    constexpr int kPer = kSaMaxSeq / kThreads;   // sequences a thread counts, in order
-    int mine = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        const int b = tid * kPer + i;
-        if (b < a.n_seq) mine += ceil_div(max(shared_len(a, b), 0), kSaTok);
-    }
-    int upto = mine;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, upto, o);
-        if (lane >= o) upto += x;
-    }
-    if (lane == 31) s_scan[warp] = upto;
-    if (tid == 0) { s_seq = a.n_seq; s_before = 0; }
-    __syncthreads();
-    int64_t c_tiles = 0, ahead = upto - mine;
-#pragma unroll
-    for (int w = 0; w < S::warps; ++w) {
-        if (w < warp) ahead += s_scan[w];
-        c_tiles += s_scan[w];
-    }
-    const int64_t total = p_total + c_tiles * seq_segs;
-    const int workers = shared_workers(total, a.ctas);
-    if ((int)blockIdx.x >= workers) return;
-    const int64_t t0 = shared_first_tile(total, workers, blockIdx.x), t1 = shared_first_tile(total, workers, blockIdx.x + 1);
-    // the sequence that the first tile falls into (if it is none of the prefix's), found by the thread that counted it
-    if (t0 >= p_total) {
-        const int64_t at = (t0 - p_total) / seq_segs;    // in tiles of sequences: a sequence's segments are equally long
-        if (at >= ahead && at < ahead + mine) {
-            int64_t before = ahead;
-            for (int i = 0; i < kPer; ++i) {
-                const int b = tid * kPer + i, n = b < a.n_seq ? ceil_div(max(shared_len(a, b), 0), kSaTok) : 0;
-                if (at < before + n) { s_seq = b; s_before = (int)before; break; }
-                before += n;
-            }
-        }
-    }
-    __syncthreads();
-
-    auto first_of_seq = [&](SaSegment& g, int b, int64_t begin) {     // segment 0 of the first sequence >= b that has tiles
-        int n = 0;
-        for (; b < a.n_seq; ++b) {
-            n = shared_len(a, b);
-            if (n > 0) break;
-        }
-        g.seq = b; g.n = n; g.index = p_segs + b * seq_segs; g.head = 0; g.first = 0;
-        g.begin = begin; g.end = begin + ceil_div(n, kSaTok);
-    };
-    auto next = [&](SaSegment& g) {
-        if (++g.head == a.n_kv) { g.head = 0; g.first += S::pairs; }
-        ++g.index;
-        if (g.seq < 0) {
-            if (g.index == p_segs) { first_of_seq(g, 0, g.end); return; }
-        } else if ((g.index - p_segs) % seq_segs == 0) {
-            first_of_seq(g, g.seq + 1, g.end);
-            return;
-        }
-        const int64_t len = g.end - g.begin;
-        g.begin = g.end;
-        g.end += len;
-    };
-    SaSegment cur;
-    if (t0 < p_total) {
-        const int i = (int)(t0 / p_tiles);
-        cur = {i, i % a.n_kv, i / a.n_kv * S::pairs, -1, a.prefix, (int64_t)i * p_tiles, (int64_t)(i + 1) * p_tiles};
-    } else {
-        first_of_seq(cur, s_seq, p_total + (int64_t)s_before * seq_segs);
-        const int64_t len = cur.end - cur.begin;
-        const int i = (int)((t0 - cur.begin) / len);     // its segment
-        cur.index += i; cur.head = i % a.n_kv; cur.first = i / a.n_kv * S::pairs;
-        cur.begin += i * len; cur.end += i * len;
-    }
-
-    // ---- copies: tile t of segment g into its stage, the segment's Q with the first of its tiles here ----
-    SaSegment ld = cur;
-    int ld_segs = 0;                                     // segments begun by the copies
-    auto pairs_of = [&](const SaSegment& g) { return (g.seq < 0 ? a.n_seq : 1) * a.rows * a.group; };
-    auto q_row = [&](const SaSegment& g, int p) {        // query of pair p of the segment's sequences
-        const int r = p / a.group, hq = g.head * a.group + p - r * a.group;
-        return a.q + (g.seq < 0 ? (int64_t)(r / a.rows) * a.q_seq + (int64_t)(r % a.rows) * a.q_row : (int64_t)g.seq * a.q_seq + (int64_t)r * a.q_row) +
-               (int64_t)hq * a.q_head;
-    };
-    auto load = [&](int64_t t) {
-        if (t < t1) {
-            if (t >= ld.end) next(ld);
-            if (t == t0 || t == ld.begin) {
-                uint8_t* to = sQ + (ld_segs % S::q_bufs) * S::q_bytes;
-                const int P = pairs_of(ld);
-                for (int i = tid; i < S::pairs * (D / 8); i += kThreads) {
-                    const int p = i / (D / 8), c = i % (D / 8);
-                    const bool there = ld.first + p < P;
-                    cp16(to + sa_at<D>(p, c), there ? q_row(ld, ld.first + p) + c * 8 : a.q, there);
-                }
-                ++ld_segs;
-            }
-            uint8_t* to = smem + (int)((t - t0) % S::stages) * S::stage_bytes;
-            const int pos0 = (int)(t - ld.begin) * kSaTok;
-            const uint16_t *k, *v;
-            int64_t stride;
-            if (ld.seq < 0) { k = a.kp + ld.head * a.p_head; v = a.vp + ld.head * a.p_head; stride = a.p_pos; }
-            else {
-                const int64_t o = ld.seq * a.c_seq + ld.head * a.c_head;
-                k = a.kc + o; v = a.vc + o; stride = a.c_pos;
-            }
-#pragma unroll 4
-            for (int i = tid; i < kSaTok * (D / 8); i += kThreads) {
-                const int p = i / (D / 8), c = i % (D / 8);
-                const bool there = pos0 + p < ld.n;
-                const int64_t o = there ? (int64_t)(pos0 + p) * stride + c * 8 : 0;
-                cp16(to + sa_at<D>(p, c), k + o, there);
-                cp16(to + kSaTok * D * 2 + sa_at<D>(p, c), v + o, there);
-            }
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");
-    };
-#pragma unroll
-    for (int i = 0; i < S::stages - 1; ++i) load(t0 + i);
-
-    // ---- products ----
-    float o[D / 8][4], m[2], l[2];
-    uint32_t qf[S::q_regs ? D / 16 : 1][4];
-    int lim[2], cur_segs = 0;                            // positions that this thread's two rows see
-    const int row = lane >> 2, col = 2 * (lane & 3);
-    for (int64_t t = t0; t < t1; ++t) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(S::stages - 2) : "memory");
-        __syncthreads();
-        const uint32_t sK = smem_u32(smem + (int)((t - t0) % S::stages) * S::stage_bytes), sV = sK + kSaTok * D * 2;
-        if (t >= cur.end) { next(cur); ++cur_segs; }
-        const uint32_t q_at = smem_u32(sQ + (cur_segs % S::q_bufs) * S::q_bytes);
-        const int q_r = mt * 16 + (lane & 15), q_c = lane >> 4;
-        if (t == t0 || t == cur.begin) {
-            if (S::q_regs) {
-#pragma unroll
-                for (int k = 0; k < D / 16; ++k) ldm4(qf[k], q_at + sa_at<D>(q_r, 2 * k + q_c));
-                __syncthreads();                         // its buffer may be filled again
-            }
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                m[i] = -INFINITY;
-                l[i] = 0.f;
-                const int p = cur.first + mt * 16 + row + 8 * i;
-                lim[i] = p >= pairs_of(cur) ? 0 : cur.seq < 0 ? a.prefix : cur.n - (a.rows - 1 - p / a.group);
-            }
-        }
-        load(t + S::stages - 1);                         // into the stage that was read before the barrier
-        const int pos0 = (int)(t - cur.begin) * kSaTok + grp * S::tok;         // this warp's first position
-        float s[S::tok / 8][4];
-#pragma unroll
-        for (int j = 0; j < S::tok / 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[j][i] = 0.f;
-#pragma unroll
-        for (int k = 0; k < D / 16; ++k) {
-            uint32_t q[4];
-            if (S::q_regs) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = qf[k][i];
-            } else {
-                ldm4(q, q_at + sa_at<D>(q_r, 2 * k + q_c));
-            }
-#pragma unroll
-            for (int j = 0; j < S::tok / 16; ++j) {
-                uint32_t b[4];                           // positions 0-7 and 8-15, eight dims each twice
-                ldm4(b, sK + sa_at<D>(grp * S::tok + j * 16 + (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
-                T::mma(s[2 * j], q, b[0], b[1]);
-                T::mma(s[2 * j + 1], q, b[2], b[3]);
-            }
-        }
-        const bool cut = pos0 + S::tok > min(lim[0], lim[1]);
-#pragma unroll
-        for (int j = 0; j < S::tok / 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[j][i] *= a.scale_log2;
-                if (cut && pos0 + j * 8 + col + (i & 1) >= lim[i >> 1]) s[j][i] = -INFINITY;
-            }
-        if (a.scores && cur.seq >= 0) {
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int p = cur.first + mt * 16 + row + 8 * i;
-                if (p >= a.rows * a.group) continue;
-                float* to = a.scores + (((int64_t)cur.seq * a.n_kv + cur.head) * a.rows * a.group + p) * a.capacity;
-#pragma unroll
-                for (int j = 0; j < S::tok / 8; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int pos = pos0 + j * 8 + col + e;
-                        if (pos < cur.n) to[pos] = s[j][2 * i + e];
-                    }
-            }
-        }
-        float base[2], fix[2];
-        bool grew = false;
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            float x = m[i];
-#pragma unroll
-            for (int j = 0; j < S::tok / 8; ++j) x = fmaxf(x, fmaxf(s[j][2 * i], s[j][2 * i + 1]));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 1));
-            x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, 2));
-            base[i] = x == -INFINITY ? 0.f : x;
-            fix[i] = exp2_fast(m[i] - base[i]);
-            grew |= x != m[i];
-            m[i] = x;
-        }
-        if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-            for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[i][j] *= fix[j >> 1];
-            l[0] *= fix[0];
-            l[1] *= fix[1];
-        }
-#pragma unroll
-        for (int j = 0; j < S::tok / 8; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                s[j][i] = exp2_fast(s[j][i] - base[i >> 1]);
-                l[i >> 1] += s[j][i];
-            }
-        // Positions that some of the warp's rows do not see: what is no number in their V must not meet a 0 of P in the product.
-        // It is taken out there and added, for the rows that see it, one by one.
-        const int seen_by_all = cur.seq < 0 ? a.prefix : cur.n - (a.rows - 1);
-        const bool guard = pos0 + S::tok > seen_by_all && pos0 < cur.n && a.rows > 1 && cur.seq >= 0;
-#pragma unroll
-        for (int j = 0; j < S::tok / 16; ++j) {
-            const uint32_t p[4] = {T::pack(s[2 * j][0], s[2 * j][1]), T::pack(s[2 * j][2], s[2 * j][3]), T::pack(s[2 * j + 1][0], s[2 * j + 1][1]),
-                                   T::pack(s[2 * j + 1][2], s[2 * j + 1][3])};
-#pragma unroll
-            for (int n = 0; n < D / 16; ++n) {
-                uint32_t b[4];                           // dims 0-7 (16 positions), dims 8-15
-                ldm4_t(b, sV + sa_at<D>(grp * S::tok + j * 16 + (lane & 15), 2 * n + (lane >> 4)));
-                if (guard) {
-                    bool odd = false;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if ((b[i] & T::kExponent) == T::kExponent) { b[i] &= 0xFFFF0000u; odd = true; }
-                        if ((b[i] >> 16 & T::kExponent) == T::kExponent) { b[i] &= 0x0000FFFFu; odd = true; }
-                    }
-                    if (__any_sync(0xffffffffu, odd)) {
-                        for (int k = 0; k < 16; ++k) {   // position by position; p of (row, k) is in lane 4 row + (k % 8) / 2
-                            const int pos = pos0 + j * 16 + k, src = (lane & ~3) | ((k & 7) >> 1);
-                            float x[2];
-#pragma unroll
-                            for (int i = 0; i < 2; ++i) {
-                                const float even = __shfl_sync(0xffffffffu, k < 8 ? s[2 * j][2 * i] : s[2 * j + 1][2 * i], src);
-                                const float oddp = __shfl_sync(0xffffffffu, k < 8 ? s[2 * j][2 * i + 1] : s[2 * j + 1][2 * i + 1], src);
-                                x[i] = (k & 1) ? oddp : even;
-                            }
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                const uint32_t at = sV + sa_at<D>(grp * S::tok + j * 16 + k, 2 * n + h) + col * 2;
-                                uint32_t w;
-                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at));
-#pragma unroll
-                                for (int e = 0; e < 2; ++e) {
-                                    const uint32_t bits = e ? w >> 16 : w & 0xFFFFu;
-                                    if ((bits & T::kExponent) != T::kExponent) continue;
-#pragma unroll
-                                    for (int i = 0; i < 2; ++i)
-                                        if (pos < lim[i]) o[2 * n + h][2 * i + e] = fmaf(x[i], T::get(bits), o[2 * n + h][2 * i + e]);
-                                }
-                            }
-                        }
-                    }
-                }
-                T::mma(o[2 * n], p, b[0], b[1]);
-                T::mma(o[2 * n + 1], p, b[2], b[3]);
-            }
-        }
-        // ---- the segment's end, or the worker's: join the warps' positions, through the stage that was read last ----
-        if (t + 1 == t1 || t + 1 == cur.end) {
-            __syncthreads();
-            float* box = reinterpret_cast<float*>(smem + (int)((t - t0) % S::stages) * S::stage_bytes);
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
-                l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
-                if ((lane & 3) == 0) {
-                    s_ml[grp][mt * 16 + row + 8 * i][0] = m[i];
-                    s_ml[grp][mt * 16 + row + 8 * i][1] = l[i];
-                }
-            }
-            if (grp > 0) {
-                float4* to = reinterpret_cast<float4*>(box) + ((grp - 1) * MT + mt) * (D / 8) * 32 + lane;
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i) to[i * 32] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-            }
-            __syncthreads();
-            if (grp == 0) {
-                float all[2] = {-INFINITY, -INFINITY}, sum[2] = {0.f, 0.f}, w[S::groups][2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int p = mt * 16 + row + 8 * i;
-#pragma unroll
-                    for (int g = 0; g < S::groups; ++g) all[i] = fmaxf(all[i], s_ml[g][p][0]);
-                    const float b = all[i] == -INFINITY ? 0.f : all[i];
-#pragma unroll
-                    for (int g = 0; g < S::groups; ++g) {
-                        w[g][i] = exp2_fast(s_ml[g][p][0] - b);
-                        sum[i] += w[g][i] * s_ml[g][p][1];
-                    }
-                }
-#pragma unroll
-                for (int i = 0; i < D / 8; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[i][j] *= w[0][j >> 1];
-#pragma unroll
-                for (int g = 1; g < S::groups; ++g) {
-                    const float4* from = reinterpret_cast<const float4*>(box) + ((g - 1) * MT + mt) * (D / 8) * 32 + lane;
-#pragma unroll
-                    for (int i = 0; i < D / 8; ++i) {
-                        const float4 x = from[i * 32];
-                        o[i][0] = fmaf(w[g][0], x.x, o[i][0]);
-                        o[i][1] = fmaf(w[g][0], x.y, o[i][1]);
-                        o[i][2] = fmaf(w[g][1], x.z, o[i][2]);
-                        o[i][3] = fmaf(w[g][1], x.w, o[i][3]);
-                    }
-                }
-                const int64_t slot = (int64_t)blockIdx.x + cur.index;
-                const int P = min(pairs_of(cur) - cur.first, S::pairs);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int p = mt * 16 + row + 8 * i;
-                    if (p >= P) continue;
-                    float* to = a.part_o + (slot * a.pairs + p) * D + col;
-#pragma unroll
-                    for (int j = 0; j < D / 8; ++j) *reinterpret_cast<float2*>(to + j * 8) = make_float2(o[j][2 * i], o[j][2 * i + 1]);
-                    if ((lane & 3) == 0) {
-                        a.part_m[slot * a.pairs + p] = all[i];
-                        a.part_l[slot * a.pairs + p] = sum[i];
-                    }
-                }
-            }
-        }
-    }
-}
 
 // ---- joining the parts ----
 constexpr int kSmThreads = 128, kSmWarps = kSmThreads / 32;
@@ -532,30 +93,31 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     before = __reduce_add_sync(0xffffffffu, before);
     tiles = __reduce_add_sync(0xffffffffu, tiles);
 
-    // maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M)
-    auto sums = [&](const SaParts& s, float* w, float& M, float& L) {
-        const float *pm = s.pre_tc ? a.pre_m : a.part_m, *pl = s.pre_tc ? a.pre_l : a.part_l;
+    // Maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M).  The first 32 are loaded ahead.
+    auto load = [&](const SaParts& s, int i, float& m, float& l) {
+        m = -INFINITY;
+        l = 0.f;
+        if (i >= s.count()) return;
+        const bool pre = i < s.n_pre;
+        const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * s.own_step;
+        m = (pre && s.pre_tc ? a.pre_m : a.part_m)[at];
+        l = (pre && s.pre_tc ? a.pre_l : a.part_l)[at];
+    };
+    auto sums = [&](const SaParts& s, float m0, float l0, float* w, float& M, float& L) {
         const int count = s.count();
-        float m0 = -INFINITY, l0 = 0.f;                  // of the first 32, one round trip
-        auto load = [&](int i, float& m, float& l) {
-            if (i < s.n_pre) { m = pm[s.pre0 + i * s.pre_step]; l = pl[s.pre0 + i * s.pre_step]; }
-            else { const int64_t at = s.own0 + (int64_t)(i - s.n_pre) * s.own_step; m = a.part_m[at]; l = a.part_l[at]; }
-        };
-        if (lane < count) load(lane, m0, l0);
         M = m0;
         for (int i = lane + 32; i < count; i += 32) {
             float m, l;
-            load(i, m, l);
+            load(s, i, m, l);
             M = fmaxf(M, m);
         }
         M = warp_max(M);
-        const float base = M == -INFINITY ? 0.f : M;
-        const float f0 = exp2_fast(m0 - base);
+        const float base = M == -INFINITY ? 0.f : M, f0 = exp2_fast(m0 - base);
         L = f0 * l0;
         if (w && lane < count) w[lane] = f0;
         for (int i = lane + 32; i < count; i += 32) {
             float m, l;
-            load(i, m, l);
+            load(s, i, m, l);
             const float f = exp2_fast(m - base);
             L += f * l;
             if (w) w[i] = f;
@@ -564,37 +126,59 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
         __syncwarp();
     };
     if (weights) {
-        const int pos0 = chunk * kSmPos;
+        const int pos = chunk * kSmPos + tid * 4;
         const float* in = weight_in ? weight_in + ((int64_t)b * a.n_kv + head) * a.capacity : nullptr;
         float* to = weight_out + ((int64_t)b * a.n_kv + head) * a.capacity;
         float* s_lse = &s_w[0][0];
-        if (pos0 < n) {
-            for (int q = warp; q < P; q += kSmWarps) {
-                float M, L;
-                sums(shared_parts(a, seg_pairs, b, head, q, before, tiles, n), nullptr, M, L);
-                if (lane == 0) s_lse[q] = M + log2f(L);
+        float sum[4] = {0.f, 0.f, 0.f, 0.f}, was[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) was[i] = in && pos + i < a.capacity ? in[pos + i] : 0.f;
+        if (chunk * kSmPos < n) {
+            constexpr int kBatch = 4;                    // pairs of a warp under way
+            for (int q0 = warp; q0 < P; q0 += kSmWarps * kBatch) {
+                SaParts s[kBatch];
+                float m[kBatch], l[kBatch];
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    s[i] = shared_parts(a, seg_pairs, b, head, min(q0 + i * kSmWarps, P - 1), before, tiles, n);
+                    load(s[i], lane, m[i], l[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < kBatch; ++i) {
+                    float M, L;
+                    sums(s[i], m[i], l[i], nullptr, M, L);
+                    if (lane == 0 && q0 + i * kSmWarps < P) s_lse[q0 + i * kSmWarps] = M + log2f(L);
+                }
             }
             __syncthreads();
-        }
-        const float* from = a.scores + ((int64_t)b * a.n_kv + head) * P * a.capacity;
+            const float* from = a.scores + ((int64_t)b * a.n_kv + head) * P * a.score_stride + pos;
+            for (int q0 = 0; q0 < P; q0 += 8) {
+                float4 x[8];
 #pragma unroll
-        for (int i = 0; i < kSmPos / kSmThreads; ++i) {
-            const int pos = pos0 + i * kSmThreads + tid;
-            if (pos >= a.capacity) break;
-            float sum = 0.f;
-            for (int q = 0; q < a.rows; ++q) {
-                if (pos >= n - (a.rows - 1 - q)) continue;
-                for (int g = 0; g < a.group; ++g) sum += exp2_fast(from[(int64_t)(q * a.group + g) * a.capacity + pos] - s_lse[q * a.group + g]);
+                for (int i = 0; i < 8; ++i)
+                    if (q0 + i < P && pos < n) x[i] = *reinterpret_cast<const float4*>(from + (q0 + i) * a.score_stride);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    if (q0 + i >= P) continue;
+                    const int end = n - (a.rows - 1 - (q0 + i) / a.group);           // what the pair sees
+                    const float z = s_lse[q0 + i], v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (pos + e < end) sum[e] += exp2_fast(v[e] - z);
+                }
             }
-            if (pos < n || in != to) to[pos] = (in ? in[pos] : 0.f) + sum;
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (pos + i < a.capacity && (pos + i < n || in != to)) to[pos + i] = was[i] + sum[i];
         return;
     }
     if (p == 0 && head == 0 && warp % WARPS == 0 && lane == 0 && a.lens && a.lens[b] > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
     const SaParts s = shared_parts(a, seg_pairs, b, head, p, before, tiles, n);
     const int parts = s.count();
-    float M, L, *w = s_w[warp];
-    sums(s, w, M, L);                                    // each of the pair's warps for itself
+    float M, L, m0, l0, *w = s_w[warp];
+    load(s, lane, m0, l0);
+    sums(s, m0, l0, w, M, L);                            // each of the pair's warps for itself
     const float* po = s.pre_tc ? a.pre_o : a.part_o;
     const bool sees = a.prefix > 0 || n - (a.rows - 1 - r) > 0;
     uint16_t* to = out + (int64_t)b * a.out_seq + (int64_t)r * a.out_row + (int64_t)hq * a.out_head;
@@ -635,7 +219,7 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
 
 struct SaPlan {
     SharedAttn a;
-    int mt, per_sm;
+    int mt;
     bool tc;
     size_t at_o, at_m, at_l, at_scores, at_pre_o, at_pre_m, at_pre_l, bytes;
 };
@@ -677,8 +261,8 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     a.pairs = most < seg ? most : seg;
     a.p_groups = a.prefix && !plan->tc ? ceil_div(all, seg) : 0;
     a.c_groups = ceil_div(P, seg);
-    plan->per_sm = plan->mt == 4 || a.d > 128 ? 1 : 2;
-    a.ctas = kSms * plan->per_sm;
+    a.ctas = kSms * shared_stream_per_sm(a.d, plan->mt);
+    a.score_stride = (int64_t)align_up(a.capacity, 4);
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o2 = off; off = align_up(off + b, 256); return o2; };
     const size_t slots = (size_t)a.ctas + (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups);
@@ -689,27 +273,9 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     plan->at_pre_o = take(pre * a.d * 4);
     plan->at_pre_m = take(pre * 4);
     plan->at_pre_l = take(pre * 4);
-    plan->at_scores = take(with_weights ? (size_t)a.n_seq * a.n_q * a.rows * a.capacity * 4 : 0);
+    plan->at_scores = take(with_weights ? (size_t)a.n_seq * a.n_q * a.rows * a.score_stride * 4 : 0);
     plan->bytes = off < 256 ? 256 : off;
     return CASS_OK;
-}
-
-template <int DT, int D, int MT>
-static int run_stream(const SharedAttn& a, cudaStream_t s) {
-    using S = SaShape<D, MT>;
-    CASS_ALLOW_SMEM(k_shared_stream<DT, D, MT>);
-    CASS_PDL_LAUNCH((k_shared_stream<DT, D, MT>), dim3(a.ctas), dim3(S::warps * 32), (size_t)S::smem, s, a);
-    return CASS_OK;
-}
-
-template <int DT, int D>
-static int run_stream_d(const SharedAttn& a, int mt, cudaStream_t s) {
-    if (mt == 1) return run_stream<DT, D, 1>(a, s);
-    if constexpr (D <= 128) {
-        if (mt == 2) return run_stream<DT, D, 2>(a, s);
-        if (mt == 4) return run_stream<DT, D, 4>(a, s);
-    }
-    return CASS_ERR_UNSUPPORTED;
 }
 
 template <int DT>
@@ -717,15 +283,7 @@ static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float
     const SharedAttn& a = plan.a;
     int rc = plan.tc ? launch_shared_prefix_tc(a, DT, d_status, s) : CASS_OK;
     if (rc) return rc;
-    rc = CASS_ERR_UNSUPPORTED;
-    switch (a.d) {
-        case 32: rc = run_stream_d<DT, 32>(a, plan.mt, s); break;
-        case 64: rc = run_stream_d<DT, 64>(a, plan.mt, s); break;
-        case 96: rc = run_stream_d<DT, 96>(a, plan.mt, s); break;
-        case 128: rc = run_stream_d<DT, 128>(a, plan.mt, s); break;
-        case 192: rc = run_stream_d<DT, 192>(a, plan.mt, s); break;
-        case 256: rc = run_stream_d<DT, 256>(a, plan.mt, s); break;
-    }
+    rc = DT == CASS_BF16 ? launch_shared_stream_bf16(a, plan.mt, d_status, s) : launch_shared_stream_f16(a, plan.mt, d_status, s);
     if (rc) return rc;
     const int pos_blocks = weight_out ? ceil_div(a.capacity, kSmPos) : 0;
     const int64_t pairs = (int64_t)a.n_seq * a.rows * a.n_q;

@@ -1,9 +1,48 @@
 // What the kernels of the shared-prefix attention have in common: sizes, addresses, where partial results lie.
 #pragma once
 
+#include <cuda_fp16.h>
+
 #include "kernels.cuh"
 
 namespace cass {
+
+// ---- 16-bit types ----
+template <int DT> struct SaType;
+template <> struct SaType<CASS_BF16> {
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static constexpr uint32_t kExponent = 0x7F80u;
+    static __device__ __forceinline__ float get(uint32_t v) { return __uint_as_float(v << 16); }
+    static __device__ __forceinline__ uint16_t put(float v) { return float_to_bf16_bits(v); }
+};
+template <> struct SaType<CASS_F16> {
+    static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
+        uint32_t r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+        return r;
+    }
+    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    static constexpr uint32_t kExponent = 0x7C00u;
+    static __device__ __forceinline__ float get(uint32_t v) { return __half2float(__ushort_as_half((uint16_t)v)); }
+    static __device__ __forceinline__ uint16_t put(float v) { return __half_as_ushort(__float2half_rn(v)); }
+};
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
 
 constexpr int kSaTok = 64;                               // positions of a tile of the streaming kernel
 constexpr int kSaMaxSeq = 1024;
@@ -16,7 +55,8 @@ struct SharedAttn {
     const int32_t* lens;
     // scratch.  A part: the unnormalised output, maximum and sum of up to `pairs` (row, query head) pairs over some positions.
     float *part_o, *part_m, *part_l;                     // [slot][pairs][d], [slot][pairs], [slot][pairs]
-    float* scores;                                       // [sequence][query head x row in pair order][capacity], for the weights; or null
+    float* scores;                                       // [sequence][KV head][pair][score_stride], for the weights; or null
+    int64_t score_stride;                                // the capacity, rounded up to 4
     // the streaming kernel's work
     int ctas, pairs;                                     // CTAs; pairs of a segment
     int p_groups, c_groups;                              // segments of pairs of the prefix (0: not this kernel's) and of a sequence
@@ -46,6 +86,10 @@ __device__ __forceinline__ int shared_workers(int64_t tiles, int ctas) { return 
 __device__ __forceinline__ int64_t shared_first_tile(int64_t tiles, int workers, int w) { return tiles * w / workers; }
 __device__ __forceinline__ int shared_worker_of(int64_t tiles, int workers, int64_t t) { return (int)(((t + 1) * workers - 1) / tiles); }
 
+// mt: tiles of 16 pairs that a CTA takes at a time, 1, 2 or 4 (1 beyond head size 128)
+inline int shared_stream_per_sm(int d, int mt) { return mt == 1 && d <= 128 ? 2 : 1; }          // CTAs an SM holds
+int launch_shared_stream_bf16(const SharedAttn& a, int mt, int32_t* d_status, cudaStream_t s);
+int launch_shared_stream_f16(const SharedAttn& a, int mt, int32_t* d_status, cudaStream_t s);
 int launch_shared_prefix_tc(const SharedAttn& a, int dtype, int32_t* d_status, cudaStream_t s);
 
 }  // namespace cass
