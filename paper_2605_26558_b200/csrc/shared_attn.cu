@@ -14,21 +14,18 @@ constexpr int kSmPos = 4 * kSmThreads;                   // positions of a weigh
 
 // Where the parts of (sequence b, head, pair p of the sequence) lie: those of the prefix, then those of its cache, in order.
 struct SaParts {
-    int64_t pre0, pre_step, own0;                        // first place, distance of two, in pairs
-    int n_pre, n_own, own_step;
+    int64_t pre0, own0, pre_step;                        // first places, distance of two of the prefix (of the cache: a.pairs), in pairs
+    int n_pre, n_own;
     bool pre_tc;
     __device__ __forceinline__ int count() const { return n_pre + n_own; }
 };
 
-__device__ SaParts shared_parts(const SharedAttn& a, int seg_pairs, int b, int head, int p, int tiles_before, int64_t c_tiles, int n) {
+__device__ SaParts shared_parts(const SharedAttn& a, const SaList& list, int seg_pairs, int b, int head, int p, int tiles_before, int n) {
     SaParts r{};
-    const int p_tiles = a.p_groups ? ceil_div(a.prefix, kSaTok) : 0, seq_segs = a.c_groups * a.n_kv, p_segs = a.p_groups * a.n_kv;
-    const int64_t p_total = (int64_t)p_tiles * p_segs, total = p_total + c_tiles * seq_segs;
-    const int workers = shared_workers(total, a.ctas);
-    const int P = a.rows * a.group, all = b * P + p;     // the pair among those of all sequences
-    if (p_tiles) {
+    const int all = b * a.rows * a.group + p;            // the pair among those of all sequences
+    if (list.p_tiles) {
         const int s = all / seg_pairs * a.n_kv + head;
-        const int w0 = shared_worker_of(total, workers, (int64_t)s * p_tiles), w1 = shared_worker_of(total, workers, (int64_t)(s + 1) * p_tiles - 1);
+        const int w0 = shared_worker_of(list, s * list.p_tiles), w1 = shared_worker_of(list, (s + 1) * list.p_tiles - 1);
         r.pre0 = (int64_t)(w0 + s) * a.pairs + all % seg_pairs;
         r.pre_step = a.pairs;
         r.n_pre = w1 - w0 + 1;
@@ -47,11 +44,9 @@ __device__ SaParts shared_parts(const SharedAttn& a, int seg_pairs, int b, int h
     }
     const int tiles = ceil_div(max(n, 0), kSaTok);
     if (tiles) {
-        const int k = p / seg_pairs * a.n_kv + head;
-        const int64_t first = p_total + (int64_t)tiles_before * seq_segs + (int64_t)k * tiles;
-        const int w0 = shared_worker_of(total, workers, first), w1 = shared_worker_of(total, workers, first + tiles - 1);
-        r.own0 = (int64_t)(w0 + p_segs + b * seq_segs + k) * a.pairs + p % seg_pairs;
-        r.own_step = a.pairs;
+        const int k = p / seg_pairs * a.n_kv + head, first = list.p_total + tiles_before * list.seq_segs + k * tiles;
+        const int w0 = shared_worker_of(list, first), w1 = shared_worker_of(list, first + tiles - 1);
+        r.own0 = (int64_t)(w0 + list.p_segs + b * list.seq_segs + k) * a.pairs + p % seg_pairs;
         r.n_own = w1 - w0 + 1;
     }
     return r;
@@ -67,8 +62,6 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     __shared__ float s_w[kSmWarps][kSmMaxParts];
     __shared__ __align__(16) float s_o[kSmWarps][256];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    pdl_wait();
-    pdl_early<3>();
     const int P = a.rows * a.group;
     const bool weights = (int)blockIdx.x >= pair_blocks;
     int b, head, p = 0, r = 0, hq = 0, chunk = 0;
@@ -79,11 +72,11 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     } else {
         const int i = blockIdx.x * (kSmWarps / WARPS) + warp / WARPS;
         hq = i % a.n_q; r = i / a.n_q % a.rows; b = i / a.n_q / a.rows;
-        if (b >= a.n_seq) return;
+        if (b >= a.n_seq) { pdl_wait(); return; }
         head = hq / a.group; p = r * a.group + hq % a.group;
     }
+    // The lengths were complete before the streaming kernel released this one: where the parts lie is known by the time they are there.
     const int n = shared_len(a, b);
-    if (n < 0) return;                                   // the sequence is not there
     int before = 0, tiles = 0;
     for (int i = lane; i < a.n_seq; i += 32) {
         const int t = ceil_div(max(shared_len(a, i), 0), kSaTok);
@@ -92,6 +85,10 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     }
     before = __reduce_add_sync(0xffffffffu, before);
     tiles = __reduce_add_sync(0xffffffffu, tiles);
+    const SaList list = shared_list(a, tiles);
+    const SaParts s = shared_parts(a, list, seg_pairs, b, head, p, before, n);
+    pdl_wait();
+    if (n < 0) return;                                   // the sequence is not there
 
     // Maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M).  The first 32 are loaded ahead.
     auto load = [&](const SaParts& s, int i, float& m, float& l) {
@@ -99,7 +96,7 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
         l = 0.f;
         if (i >= s.count()) return;
         const bool pre = i < s.n_pre;
-        const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * s.own_step;
+        const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * a.pairs;
         m = (pre && s.pre_tc ? a.pre_m : a.part_m)[at];
         l = (pre && s.pre_tc ? a.pre_l : a.part_l)[at];
     };
@@ -126,7 +123,7 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
         __syncwarp();
     };
     if (weights) {
-        const int pos = chunk * kSmPos + tid * 4;
+        const int pos = chunk * kSmPos + tid * 4, per_group = list.p_tiles ? seg_pairs : 2 * kStTile;
         const float* in = weight_in ? weight_in + ((int64_t)b * a.n_kv + head) * a.capacity : nullptr;
         float* to = weight_out + ((int64_t)b * a.n_kv + head) * a.capacity;
         float* s_lse = &s_w[0][0];
@@ -134,21 +131,14 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
 #pragma unroll
         for (int i = 0; i < 4; ++i) was[i] = in && pos + i < a.capacity ? in[pos + i] : 0.f;
         if (chunk * kSmPos < n) {
-            constexpr int kBatch = 4;                    // pairs of a warp under way
-            for (int q0 = warp; q0 < P; q0 += kSmWarps * kBatch) {
-                SaParts s[kBatch];
-                float m[kBatch], l[kBatch];
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    s[i] = shared_parts(a, seg_pairs, b, head, min(q0 + i * kSmWarps, P - 1), before, tiles, n);
-                    load(s[i], lane, m[i], l[i]);
-                }
-#pragma unroll
-                for (int i = 0; i < kBatch; ++i) {
-                    float M, L;
-                    sums(s[i], m[i], l[i], nullptr, M, L);
-                    if (lane == 0 && q0 + i * kSmWarps < P) s_lse[q0 + i * kSmWarps] = M + log2f(L);
-                }
+            for (int q = warp; q < P; q += kSmWarps) {
+                SaParts t = s;                           // of pair 0: those of its neighbours lie beside them, up to the next group's
+                if (q / seg_pairs == 0 && (b * P + q) / per_group == b * P / per_group) { t.pre0 += q; t.own0 += q; }
+                else t = shared_parts(a, list, seg_pairs, b, head, q, before, n);
+                float m, l, M, L;
+                load(t, lane, m, l);
+                sums(t, m, l, nullptr, M, L);
+                if (lane == 0) s_lse[q] = M + log2f(L);
             }
             __syncthreads();
             const float* from = a.scores + ((int64_t)b * a.n_kv + head) * P * a.score_stride + pos;
@@ -174,7 +164,6 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
         return;
     }
     if (p == 0 && head == 0 && warp % WARPS == 0 && lane == 0 && a.lens && a.lens[b] > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
-    const SaParts s = shared_parts(a, seg_pairs, b, head, p, before, tiles, n);
     const int parts = s.count();
     float M, L, m0, l0, *w = s_w[warp];
     load(s, lane, m0, l0);
@@ -191,7 +180,7 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 8
         for (int i = warp % WARPS; i < parts; i += WARPS) {
-            const float* from = i < s.n_pre ? po + (s.pre0 + i * s.pre_step) * a.d : a.part_o + (s.own0 + (int64_t)(i - s.n_pre) * s.own_step) * a.d;
+            const float* from = i < s.n_pre ? po + (s.pre0 + i * s.pre_step) * a.d : a.part_o + (s.own0 + (int64_t)(i - s.n_pre) * a.pairs) * a.d;
             const float4 x = *reinterpret_cast<const float4*>(from + c);
             const float f = w[i];
             sum.x = fmaf(f, x.x, sum.x); sum.y = fmaf(f, x.y, sum.y); sum.z = fmaf(f, x.z, sum.z); sum.w = fmaf(f, x.w, sum.w);
@@ -261,14 +250,18 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     a.pairs = most < seg ? most : seg;
     a.p_groups = a.prefix && !plan->tc ? ceil_div(all, seg) : 0;
     a.c_groups = ceil_div(P, seg);
-    a.ctas = kSms * shared_stream_per_sm(a.d, plan->mt);
+    a.ctas = kSms;
     a.score_stride = (int64_t)align_up(a.capacity, 4);
+    // (with a cache's rows apart the sum fits any memory; a prefix without tensor cores may be walked by many groups)
+    const int64_t tiles = (int64_t)a.p_groups * a.n_kv * ceil_div(a.prefix, kSaTok) + (int64_t)a.n_seq * a.n_kv * a.c_groups * (a.capacity / kSaTok + 1);
+    if (tiles > kSaMaxTiles) return CASS_ERR_UNSUPPORTED;
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o2 = off; off = align_up(off + b, 256); return o2; };
     const size_t slots = (size_t)a.ctas + (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups);
     plan->at_o = take(slots * a.pairs * a.d * 4);
     plan->at_m = take(slots * a.pairs * 4);
     plan->at_l = take(slots * a.pairs * 4);
+    a.behind_tc = plan->tc;
     const size_t pre = plan->tc ? (size_t)shared_tc_plan(a) : 0;
     plan->at_pre_o = take(pre * a.d * 4);
     plan->at_pre_m = take(pre * 4);

@@ -58,6 +58,7 @@ struct SharedAttn {
     float* scores;                                       // [sequence][KV head][pair][score_stride], for the weights; or null
     int64_t score_stride;                                // the capacity, rounded up to 4
     // the streaming kernel's work
+    int behind_tc;                                       // it is launched behind the tensor-core kernel, whose parts it does not need
     int ctas, pairs;                                     // CTAs; pairs of a segment
     int p_groups, c_groups;                              // segments of pairs of the prefix (0: not this kernel's) and of a sequence
     // The prefix by the tensor-core kernel: the pairs of all sequences in tiles of 128.  Two tiles a CTA, `pre_n2` CTAs a head, its positions over
@@ -80,14 +81,36 @@ __device__ __forceinline__ int shared_len(const SharedAttn& a, int b) {
 }
 
 // The streaming kernel's segments are numbered: those of the prefix (group, head), then those of the sequences (sequence, group,
-// head); their tiles form one list of T, worker w of W = min(T, CTAs) takes tiles w T / W to (w + 1) T / W (one at least), and its part
-// of segment s goes to slot w + s (from one part to the next either number grows, so no two share a slot).
-__device__ __forceinline__ int shared_workers(int64_t tiles, int ctas) { return (int)min(tiles, (int64_t)ctas); }
-__device__ __forceinline__ int64_t shared_first_tile(int64_t tiles, int workers, int w) { return tiles * w / workers; }
-__device__ __forceinline__ int shared_worker_of(int64_t tiles, int workers, int64_t t) { return (int)(((t + 1) * workers - 1) / tiles); }
+// head); their tiles form one list of T, of which worker w of W = min(T, CTAs) takes those from w T / W on, and its part of segment s goes
+// to slot w + s (from one part to the next either number grows, so no two share a slot).  (T / W + 1 tiles for the first T % W workers and
+// T / W for the others sets neighbours the same distance apart: one cache of 32000 positions 29 -> 35 us.)
+struct SaList {
+    int p_tiles, p_total, seq_segs, p_segs, total, workers;
+    uint64_t step;                                       // T / W in 2^-32
+};
+__device__ __forceinline__ SaList shared_list(const SharedAttn& a, int c_tiles) {      // c_tiles: tiles of all sequences' lengths
+    SaList s;
+    s.p_tiles = a.p_groups ? ceil_div(a.prefix, kSaTok) : 0;
+    s.p_segs = a.p_groups * a.n_kv;
+    s.seq_segs = a.c_groups * a.n_kv;
+    s.p_total = s.p_tiles * s.p_segs;
+    s.total = s.p_total + c_tiles * s.seq_segs;
+    s.workers = max(min(s.total, a.ctas), 1);
+    // long division, 16 bits at a time (the remainders are below the number of CTAs, below 2^16)
+    const uint32_t W = (uint32_t)s.workers, each = (uint32_t)s.total / W, r0 = ((uint32_t)s.total - each * W) << 16, q1 = r0 / W, r1 = (r0 - q1 * W) << 16;
+    s.step = ((uint64_t)each << 32) | (q1 << 16) | (r1 / W);
+    return s;
+}
+__device__ __forceinline__ int shared_first_tile(const SaList& s, int w) { return w >= s.workers ? s.total : (int)(((uint64_t)(uint32_t)w * s.step) >> 32); }
+__device__ __forceinline__ int shared_worker_of(const SaList& s, int t) {
+    int w = min((int)__fdividef((float)t * (float)s.workers, (float)s.total), s.workers - 1);      // one off at most
+    while (w > 0 && shared_first_tile(s, w) > t) --w;
+    while (shared_first_tile(s, w + 1) <= t) ++w;
+    return w;
+}
+constexpr int64_t kSaMaxTiles = 1 << 30;
 
 // mt: tiles of 16 pairs that a CTA takes at a time, 1, 2 or 4 (1 beyond head size 128)
-inline int shared_stream_per_sm(int d, int mt) { return mt == 1 && d <= 128 ? 2 : 1; }          // CTAs an SM holds
 int launch_shared_stream_bf16(const SharedAttn& a, int mt, int32_t* d_status, cudaStream_t s);
 int launch_shared_stream_f16(const SharedAttn& a, int mt, int32_t* d_status, cudaStream_t s);
 int launch_shared_prefix_tc(const SharedAttn& a, int dtype, int32_t* d_status, cudaStream_t s);

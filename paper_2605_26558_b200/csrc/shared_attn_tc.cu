@@ -158,6 +158,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
+    pdl_launch_dependents();                             // the streaming kernel, which waits for this one at its end
     if (warp < 4) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kStRegsIssue));
         if (warp == 0) {
