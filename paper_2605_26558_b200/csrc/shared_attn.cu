@@ -8,8 +8,8 @@
 namespace cass {
 
 // ---- joining the parts ----
-constexpr int kSmThreads = 128, kSmWarps = kSmThreads / 32;
-constexpr int kSmMaxParts = 4 * kSms;                // of a pair: at most every CTA's of either kernel, and two a CTA of the tensor-core kernel's
+constexpr int kSmThreads = 256, kSmWarps = kSmThreads / 32;
+constexpr int kSmMaxParts = (2 * kSaLevels + 2) * kSms;          // of a pair: at most all units', and two of every CTA of the tensor-core kernel
 constexpr int kSmPos = 4 * kSmThreads;                   // positions of a weights block
 
 // Where the parts of (sequence b, head, pair p of the sequence) lie: those of the prefix, then those of its cache, in order.
@@ -25,7 +25,7 @@ __device__ SaParts shared_parts(const SharedAttn& a, const SaList& list, int seg
     const int all = b * a.rows * a.group + p;            // the pair among those of all sequences
     if (list.p_tiles) {
         const int s = all / seg_pairs * a.n_kv + head;
-        const int w0 = shared_worker_of(list, s * list.p_tiles), w1 = shared_worker_of(list, (s + 1) * list.p_tiles - 1);
+        const int w0 = shared_unit_of(list, s * list.p_tiles), w1 = shared_unit_of(list, (s + 1) * list.p_tiles - 1);
         r.pre0 = (int64_t)(w0 + s) * a.pairs + all % seg_pairs;
         r.pre_step = a.pairs;
         r.n_pre = w1 - w0 + 1;
@@ -45,22 +45,22 @@ __device__ SaParts shared_parts(const SharedAttn& a, const SaList& list, int seg
     const int tiles = ceil_div(max(n, 0), kSaTok);
     if (tiles) {
         const int k = p / seg_pairs * a.n_kv + head, first = list.p_total + tiles_before * list.seq_segs + k * tiles;
-        const int w0 = shared_worker_of(list, first), w1 = shared_worker_of(list, first + tiles - 1);
+        const int w0 = shared_unit_of(list, first), w1 = shared_unit_of(list, first + tiles - 1);
         r.own0 = (int64_t)(w0 + list.p_segs + b * list.seq_segs + k) * a.pairs + p % seg_pairs;
         r.n_own = w1 - w0 + 1;
     }
     return r;
 }
 
-// grid: blocks of the (sequence, row, query head)s, WARPS warps each, then (with weights) one for every 512 positions of every (sequence, KV
-// head).  A warp a pair where there are many pairs, four where there are few with many parts.
+// grid: blocks of the (sequence, row, query head)s, WARPS warps each, then (with weights) one for every 1024 positions of every (sequence, KV
+// head).  A warp a pair where there are many pairs, eight where there are few with many parts.
 template <int DT, int WARPS>
 __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int seg_pairs, int pair_blocks, int pos_blocks, uint16_t* __restrict__ out,
                                                              float* __restrict__ lse, const float* weight_in, float* weight_out,
                                                              int32_t* __restrict__ d_status) {
     using T = SaType<DT>;
-    __shared__ float s_w[kSmWarps][kSmMaxParts];
-    __shared__ __align__(16) float s_o[kSmWarps][256];
+    __shared__ float s_w[WARPS == 1 ? kSmWarps : 1][kSmMaxParts];
+    __shared__ __align__(16) float s_o[WARPS == 1 ? 1 : kSmWarps][256];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int P = a.rows * a.group;
     const bool weights = (int)blockIdx.x >= pair_blocks;
@@ -90,34 +90,41 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     pdl_wait();
     if (n < 0) return;                                   // the sequence is not there
 
-    // Maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M).  The first 32 are loaded ahead.
-    auto load = [&](const SaParts& s, int i, float& m, float& l) {
-        m = -INFINITY;
-        l = 0.f;
-        if (i >= s.count()) return;
-        const bool pre = i < s.n_pre;
-        const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * a.pairs;
-        m = (pre && s.pre_tc ? a.pre_m : a.part_m)[at];
-        l = (pre && s.pre_tc ? a.pre_l : a.part_l)[at];
-    };
-    auto sums = [&](const SaParts& s, float m0, float l0, float* w, float& M, float& L) {
+    // Maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M).  What 256 parts need is loaded in one go.
+    auto sums = [&](const SaParts& s, float* w, float& M, float& L) {
         const int count = s.count();
-        M = m0;
-        for (int i = lane + 32; i < count; i += 32) {
-            float m, l;
-            load(s, i, m, l);
-            M = fmaxf(M, m);
-        }
-        M = warp_max(M);
-        const float base = M == -INFINITY ? 0.f : M, f0 = exp2_fast(m0 - base);
-        L = f0 * l0;
-        if (w && lane < count) w[lane] = f0;
-        for (int i = lane + 32; i < count; i += 32) {
-            float m, l;
-            load(s, i, m, l);
-            const float f = exp2_fast(m - base);
-            L += f * l;
-            if (w) w[i] = f;
+        const float *pm = s.pre_tc ? a.pre_m : a.part_m, *pl = s.pre_tc ? a.pre_l : a.part_l;
+        float m[8], l[8];
+        M = -INFINITY;
+        L = 0.f;
+        for (int i0 = lane; i0 - lane < count; i0 += 256) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + 32 * j;
+                m[j] = -INFINITY;
+                l[j] = 0.f;
+                if (i < count) {
+                    const bool pre = i < s.n_pre;
+                    const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * a.pairs;
+                    m[j] = (pre ? pm : a.part_m)[at];
+                    l[j] = (pre ? pl : a.part_l)[at];
+                }
+            }
+            float top = M;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top = fmaxf(top, m[j]);
+            top = warp_max(top);
+            const float base = top == -INFINITY ? 0.f : top, fix = exp2_fast(M - base);
+            if (w && M != top)                           // beyond 256 parts: the factors so far follow
+                for (int i = lane; i < i0 - lane; i += 32) w[i] *= fix;
+            L *= fix;
+            M = top;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float f = exp2_fast(m[j] - base);
+                L += f * l[j];
+                if (w && i0 + 32 * j < count) w[i0 + 32 * j] = f;
+            }
         }
         L = warp_sum(L);
         __syncwarp();
@@ -135,9 +142,8 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
                 SaParts t = s;                           // of pair 0: those of its neighbours lie beside them, up to the next group's
                 if (q / seg_pairs == 0 && (b * P + q) / per_group == b * P / per_group) { t.pre0 += q; t.own0 += q; }
                 else t = shared_parts(a, list, seg_pairs, b, head, q, before, n);
-                float m, l, M, L;
-                load(t, lane, m, l);
-                sums(t, m, l, nullptr, M, L);
+                float M, L;
+                sums(t, nullptr, M, L);
                 if (lane == 0) s_lse[q] = M + log2f(L);
             }
             __syncthreads();
@@ -165,9 +171,15 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     }
     if (p == 0 && head == 0 && warp % WARPS == 0 && lane == 0 && a.lens && a.lens[b] > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
     const int parts = s.count();
-    float M, L, m0, l0, *w = s_w[warp];
-    load(s, lane, m0, l0);
-    sums(s, m0, l0, w, M, L);                            // each of the pair's warps for itself
+    float M, L, *w = s_w[WARPS == 1 ? warp : 0];
+    if (WARPS == 1 || warp == 0) sums(s, w, M, L);
+    if (WARPS > 1) {
+        __shared__ float s_total[2];
+        if (tid == 0) { s_total[0] = M; s_total[1] = L; }
+        __syncthreads();
+        M = s_total[0];
+        L = s_total[1];
+    }
     const float* po = s.pre_tc ? a.pre_o : a.part_o;
     const bool sees = a.prefix > 0 || n - (a.rows - 1 - r) > 0;
     uint16_t* to = out + (int64_t)b * a.out_seq + (int64_t)r * a.out_row + (int64_t)hq * a.out_head;
@@ -178,12 +190,22 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
     };
     for (int c = lane * 4; c < a.d; c += 128) {
         float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-        for (int i = warp % WARPS; i < parts; i += WARPS) {
-            const float* from = i < s.n_pre ? po + (s.pre0 + i * s.pre_step) * a.d : a.part_o + (s.own0 + (int64_t)(i - s.n_pre) * a.pairs) * a.d;
-            const float4 x = *reinterpret_cast<const float4*>(from + c);
-            const float f = w[i];
-            sum.x = fmaf(f, x.x, sum.x); sum.y = fmaf(f, x.y, sum.y); sum.z = fmaf(f, x.z, sum.z); sum.w = fmaf(f, x.w, sum.w);
+        for (int i0 = warp % WARPS; i0 < parts; i0 += 8 * WARPS) {               // eight parts under way
+            float4 x[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int i = i0 + j * WARPS;
+                if (i >= parts) continue;
+                const bool pre = i < s.n_pre;
+                const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * a.pairs;
+                x[j] = *reinterpret_cast<const float4*>((pre ? po : a.part_o) + at * a.d + c);
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (i0 + j * WARPS >= parts) continue;
+                const float f = w[i0 + j * WARPS];
+                sum.x = fmaf(f, x[j].x, sum.x); sum.y = fmaf(f, x[j].y, sum.y); sum.z = fmaf(f, x[j].z, sum.z); sum.w = fmaf(f, x[j].w, sum.w);
+            }
         }
         if (WARPS == 1) put(c, sum);
         else *reinterpret_cast<float4*>(&s_o[warp][c]) = sum;
@@ -208,13 +230,13 @@ __global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int s
 
 struct SaPlan {
     SharedAttn a;
-    int mt;
+    int mt, units;                                       // units: no list that there can be has more
     bool tc;
     size_t at_o, at_m, at_l, at_scores, at_pre_o, at_pre_m, at_pre_l, bytes;
 };
 
 constexpr int kSmManyPairs = 4 * kSms;                   // joined by a warp each
-constexpr int kSaStreamPairs = 64;                       // pairs behind a prefix up to which it is streamed
+constexpr int kSaStreamPairs = 16;                       // pairs behind a prefix up to which it is streamed
 
 static bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
 
@@ -250,14 +272,15 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     a.pairs = most < seg ? most : seg;
     a.p_groups = a.prefix && !plan->tc ? ceil_div(all, seg) : 0;
     a.c_groups = ceil_div(P, seg);
-    a.ctas = kSms;
     a.score_stride = (int64_t)align_up(a.capacity, 4);
     // (with a cache's rows apart the sum fits any memory; a prefix without tensor cores may be walked by many groups)
     const int64_t tiles = (int64_t)a.p_groups * a.n_kv * ceil_div(a.prefix, kSaTok) + (int64_t)a.n_seq * a.n_kv * a.c_groups * (a.capacity / kSaTok + 1);
     if (tiles > kSaMaxTiles) return CASS_ERR_UNSUPPORTED;
+    a.ctas = kSms * shared_stream_per_sm(a.d, plan->mt);
+    plan->units = (int)(tiles < kSaLevels * a.ctas ? tiles : kSaLevels * a.ctas);
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o2 = off; off = align_up(off + b, 256); return o2; };
-    const size_t slots = (size_t)a.ctas + (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups);
+    const size_t slots = (size_t)kSaLevels * a.ctas + (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups);
     plan->at_o = take(slots * a.pairs * a.d * 4);
     plan->at_m = take(slots * a.pairs * 4);
     plan->at_l = take(slots * a.pairs * 4);
@@ -276,7 +299,7 @@ static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float
     const SharedAttn& a = plan.a;
     int rc = plan.tc ? launch_shared_prefix_tc(a, DT, d_status, s) : CASS_OK;
     if (rc) return rc;
-    rc = DT == CASS_BF16 ? launch_shared_stream_bf16(a, plan.mt, d_status, s) : launch_shared_stream_f16(a, plan.mt, d_status, s);
+    rc = DT == CASS_BF16 ? launch_shared_stream_bf16(a, plan.mt, plan.units, d_status, s) : launch_shared_stream_f16(a, plan.mt, plan.units, d_status, s);
     if (rc) return rc;
     const int pos_blocks = weight_out ? ceil_div(a.capacity, kSmPos) : 0;
     const int64_t pairs = (int64_t)a.n_seq * a.rows * a.n_q;
