@@ -87,93 +87,145 @@ __device__ __forceinline__ float2 rope_turn(int pos, double f) {
     return make_float2(n == 1 || n == 2 ? -cc : cc, n >= 2 ? -ss : ss);
 }
 
-template <class T> struct RopeType;
-template <> struct RopeType<__nv_bfloat16> {
-    static __device__ __forceinline__ float get(__nv_bfloat16 v) { return __bfloat162float(v); }
-    static __device__ __forceinline__ __nv_bfloat16 put(float v) { return __float2bfloat16_rn(v); }
+// Two neighbouring values: a 32-bit word of a 16-bit type, or two of fp32.
+template <class T> struct RopeTwo;
+template <> struct RopeTwo<__nv_bfloat16> {
+    using Raw = uint32_t;
+    static __device__ __forceinline__ float2 get(Raw w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
+    static __device__ __forceinline__ Raw put(float2 v) {
+        Raw r;
+        asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(v.y), "f"(v.x));
+        return r;
+    }
 };
-template <> struct RopeType<__half> {
-    static __device__ __forceinline__ float get(__half v) { return __half2float(v); }
-    static __device__ __forceinline__ __half put(float v) { return __float2half_rn(v); }
+template <> struct RopeTwo<__half> {
+    using Raw = uint32_t;
+    static __device__ __forceinline__ float2 get(Raw w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+    static __device__ __forceinline__ Raw put(float2 v) {
+        Raw r;
+        asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(v.y), "f"(v.x));
+        return r;
+    }
 };
-template <> struct RopeType<float> {
-    static __device__ __forceinline__ float get(float v) { return v; }
-    static __device__ __forceinline__ float put(float v) { return v; }
+template <> struct RopeTwo<float> {
+    using Raw = float2;
+    static __device__ __forceinline__ float2 get(Raw w) { return w; }
+    static __device__ __forceinline__ Raw put(float2 v) { return v; }
 };
+__device__ __forceinline__ float rope_get(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float rope_get(__half v) { return __half2float(v); }
+__device__ __forceinline__ float rope_get(float v) { return v; }
+__device__ __forceinline__ void rope_put(__nv_bfloat16& to, float v) { to = __float2bfloat16_rn(v); }
+__device__ __forceinline__ void rope_put(__half& to, float v) { to = __float2half_rn(v); }
+__device__ __forceinline__ void rope_put(float& to, float v) { to = v; }
 
-template <class T, int V> struct alignas(sizeof(T) * V) RopeVec { T v[V]; };
+template <class T, int V> struct RopeVec { struct alignas(sizeof(T) * V) Type { typename RopeTwo<T>::Raw w[V / 2]; }; };
+template <class T> struct RopeVec<T, 1> { using Type = T; };
 
 struct RopeArgs {
     cass_rope_geom g;
     int rows, per_cta;                     // rows; rows a CTA takes
     int slots, rot_slots;                  // 2 V values each: all of a head's, and those of its pairs (the rest is copied)
     int transpose;
-    uint32_t head_magic;                   // u / (query and key heads) = high half of u x magic, for u < per_cta x heads
+    int lanes, step_rows, step_heads;      // slots side by side; the distance of a thread's items
 };
 
-// A slot is V pairs, 2 V values: two vectors half a rotation apart, or side by side where pairs are interleaved or copied.
-template <class T, int V>
-__global__ void __launch_bounds__(kRopeThreads) k_rope(RopeArgs a, const double* __restrict__ freqs, const int32_t* __restrict__ positions,
-                                                       const T* q, const T* k, T* q_out, T* k_out) {
-    extern __shared__ float2 s_turn[];                                  // [per_cta][rot_dim / 2]
-    using Vec = RopeVec<T, V>;
+// A slot is V pairs, 2 V values: two vectors half a rotation apart, or side by side where pairs are interleaved (IL) or copied.
+// Sines and cosines lie as a warp's lanes read them: of two pairs together, slot after slot.
+// Single values and a runtime choice of the layout inside one kernel took 256 instructions a slot of eight pairs and its place in local
+// memory: 8191 rows of 40 half-rotated heads 73 us.
+template <class T, int V, bool IL>
+__global__ void __launch_bounds__(kRopeThreads, 4) k_rope(RopeArgs a, const double* __restrict__ freqs, const int32_t* __restrict__ positions,
+                                                          const T* q, const T* k, T* q_out, T* k_out) {
+    extern __shared__ __align__(16) float s_turn[];
+    using Vec = typename RopeVec<T, V>::Type;
     const int tid = threadIdx.x, half = a.g.rot_dim / 2, heads = a.g.n_q_heads + a.g.n_k_heads;
     const int row0 = blockIdx.x * a.per_cta, rows = min(a.per_cta, a.rows - row0);
-    const int lanes = min(a.slots, kRopeThreads), ny = kRopeThreads / lanes;     // slots side by side, (row, head)s at a time
-    const int y = tid / lanes, x0 = tid - y * lanes, total = rows * heads;
+    const int y = tid / a.lanes, x0 = tid - y * a.lanes, ny = kRopeThreads / a.lanes;
+    const int r0 = y / heads, h0 = y - r0 * heads;
+    const bool works = y < ny;
     pdl_wait();
     pdl_early<0>();
-    const double gain = freqs[half];
+    Vec vl[kRopeUnroll], vh[kRopeUnroll];
+    auto place = [&](int x, int& lo, int& hi) {                         // where the slot's two vectors begin within a head
+        const bool apart = !IL && x < a.rot_slots;
+        lo = apart ? x * V : x * 2 * V;
+        hi = apart ? half + x * V : lo + V;
+    };
+    auto step = [&](int& row, int& head) {
+        row += a.step_rows;
+        head += a.step_heads;
+        if (head >= heads) { head -= heads; ++row; }
+    };
+    auto load = [&](int x, int row, int head) {                         // kRopeUnroll items from (row, head) on
+        int lo, hi;
+        place(x, lo, hi);
+#pragma unroll
+        for (int i = 0; i < kRopeUnroll; ++i) {
+            if (row < rows) {
+                const int kh = head - a.g.n_q_heads;
+                const int64_t r = row0 + row;
+                const T* from = kh < 0 ? q + r * a.g.q_row + head * a.g.q_head : k + r * a.g.k_row + kh * a.g.k_head;
+                if (V > 1 || lo < a.g.head_dim) vl[i] = *reinterpret_cast<const Vec*>(from + lo);
+                if (V > 1 || hi < a.g.head_dim) vh[i] = *reinterpret_cast<const Vec*>(from + hi);
+            }
+            step(row, head);
+        }
+    };
+    if (works && x0 < a.slots) load(x0, r0, h0);                        // they travel while the sines are formed
+    const float gain = (float)freqs[half];
     for (int i = tid; i < rows * half; i += kRopeThreads) {
         const int r = i / half, j = i - r * half;
         float2 t = rope_turn(positions ? positions[row0 + r] : row0 + r, freqs[j]);
         if (a.transpose) t.y = -t.y;
-        s_turn[i] = make_float2(t.x * (float)gain, t.y * (float)gain);
+        const int at = V == 1 ? i : ((r * (V / 2) + j % V / 2) * a.rot_slots + j / V) * 2 + (j & 1);
+        reinterpret_cast<float2*>(s_turn)[at] = make_float2(t.x * gain, t.y * gain);
     }
     __syncthreads();
-    if (y >= ny) return;
-    for (int x = x0; x < a.slots; x += lanes) {
+    if (!works) return;
+    for (int x = x0; x < a.slots; x += a.lanes) {
         const bool turns = x < a.rot_slots;
-        // where the slot's two vectors begin within a head
-        const int lo = turns && !a.g.interleaved ? x * V : x * 2 * V, hi = turns && !a.g.interleaved ? half + x * V : lo + V;
-        const bool has_lo = V > 1 || lo < a.g.head_dim, has_hi = V > 1 || hi < a.g.head_dim;        // single values: an odd head's last
-        for (int u0 = y; u0 < total; u0 += ny * kRopeUnroll) {
-            Vec vl[kRopeUnroll], vh[kRopeUnroll];
-            T* to[kRopeUnroll];
-            int row[kRopeUnroll];
+        int lo, hi, row = r0, head = h0;
+        place(x, lo, hi);
+        while (row < rows) {
+            if (x != x0 || row != r0 || head != h0) load(x, row, head);
 #pragma unroll
             for (int i = 0; i < kRopeUnroll; ++i) {
-                const int u = u0 + i * ny;
-                to[i] = nullptr;
-                if (u >= total) continue;
-                row[i] = heads == 1 ? u : (int)__umulhi((uint32_t)u, a.head_magic);
-                const int head = u - row[i] * heads, kh = head - a.g.n_q_heads;
-                const int64_t r = row0 + row[i];
-                const T* from = kh < 0 ? q + r * a.g.q_row + head * a.g.q_head : k + r * a.g.k_row + kh * a.g.k_head;
-                to[i] = kh < 0 ? q_out + r * a.g.q_out_row + head * a.g.q_out_head : k_out + r * a.g.k_out_row + kh * a.g.k_out_head;
-                if (has_lo) vl[i] = *reinterpret_cast<const Vec*>(from + lo);
-                if (has_hi) vh[i] = *reinterpret_cast<const Vec*>(from + hi);
-            }
+                if (row < rows) {
+                    if (turns) {
+                        if constexpr (V == 1) {
+                            const float2 t = reinterpret_cast<const float2*>(s_turn)[row * half + x];
+                            const float2 r = rope_pair(rope_get(vl[i]), rope_get(vh[i]), t.x, t.y);
+                            rope_put(vl[i], r.x);
+                            rope_put(vh[i], r.y);
+                        } else {
+                            const float4* turn = reinterpret_cast<const float4*>(s_turn) + row * (V / 2) * a.rot_slots + x;
 #pragma unroll
-            for (int i = 0; i < kRopeUnroll; ++i) {
-                if (!to[i]) continue;
-                if (turns) {
-                    const float2* t = s_turn + row[i] * half + x * V;
-                    T v[2 * V];
-#pragma unroll
-                    for (int j = 0; j < V; ++j) { v[j] = vl[i].v[j]; v[V + j] = vh[i].v[j]; }
-#pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        const int ia = a.g.interleaved ? 2 * j : j, ib = a.g.interleaved ? 2 * j + 1 : V + j;
-                        const float2 y2 = rope_pair(RopeType<T>::get(v[ia]), RopeType<T>::get(v[ib]), t[j].x, t[j].y);
-                        v[ia] = RopeType<T>::put(y2.x);
-                        v[ib] = RopeType<T>::put(y2.y);
+                            for (int w = 0; w < V / 2; ++w) {
+                                const float4 t = turn[w * a.rot_slots];                  // pairs 2 w and 2 w + 1
+                                if constexpr (IL) {
+                                    // words 2 w and 2 w + 1 of the slot's V: a pair each
+                                    auto& first = 2 * w < V / 2 ? vl[i].w[2 * w % (V / 2)] : vh[i].w[2 * w % (V / 2)];
+                                    auto& second = 2 * w + 1 < V / 2 ? vl[i].w[(2 * w + 1) % (V / 2)] : vh[i].w[(2 * w + 1) % (V / 2)];
+                                    const float2 u = RopeTwo<T>::get(first), v = RopeTwo<T>::get(second);
+                                    first = RopeTwo<T>::put(rope_pair(u.x, u.y, t.x, t.y));
+                                    second = RopeTwo<T>::put(rope_pair(v.x, v.y, t.z, t.w));
+                                } else {
+                                    const float2 u = RopeTwo<T>::get(vl[i].w[w]), v = RopeTwo<T>::get(vh[i].w[w]);
+                                    const float2 e = rope_pair(u.x, v.x, t.x, t.y), f = rope_pair(u.y, v.y, t.z, t.w);
+                                    vl[i].w[w] = RopeTwo<T>::put(make_float2(e.x, f.x));
+                                    vh[i].w[w] = RopeTwo<T>::put(make_float2(e.y, f.y));
+                                }
+                            }
+                        }
                     }
-#pragma unroll
-                    for (int j = 0; j < V; ++j) { vl[i].v[j] = v[j]; vh[i].v[j] = v[V + j]; }
+                    const int kh = head - a.g.n_q_heads;
+                    const int64_t r = row0 + row;
+                    T* to = kh < 0 ? q_out + r * a.g.q_out_row + head * a.g.q_out_head : k_out + r * a.g.k_out_row + kh * a.g.k_out_head;
+                    if (V > 1 || lo < a.g.head_dim) *reinterpret_cast<Vec*>(to + lo) = vl[i];
+                    if (V > 1 || hi < a.g.head_dim) *reinterpret_cast<Vec*>(to + hi) = vh[i];
                 }
-                if (has_lo) *reinterpret_cast<Vec*>(to[i] + lo) = vl[i];
-                if (has_hi) *reinterpret_cast<Vec*>(to[i] + hi) = vh[i];
+                step(row, head);
             }
         }
     }
@@ -188,37 +240,47 @@ static bool cells_apart(int64_t rows, int64_t heads, int64_t row_stride, int64_t
     return row_stride >= inner && head_stride >= (rows - 1) * row_stride + inner;
 }
 
+template <class T, int V>
+static int run_rope(RopeArgs a, const double* freqs, const int32_t* positions, const void* q, const void* k, void* q_out, void* k_out, int copied,
+                    cudaStream_t s) {
+    const int half = a.g.rot_dim / 2, heads = a.g.n_q_heads + a.g.n_k_heads;
+    a.rot_slots = half / V;
+    a.slots = a.rot_slots + ceil_div(copied, 2 * V);
+    a.lanes = a.slots < kRopeThreads ? a.slots : kRopeThreads;
+    const int ny = kRopeThreads / a.lanes;
+    a.step_rows = ny / heads;
+    a.step_heads = ny % heads;
+    a.per_cta = half >= kRopeThreads ? 1 : kRopeThreads / half;
+    if (a.per_cta > ceil_div(a.rows, kSms)) a.per_cta = ceil_div(a.rows, kSms);      // few rows: all SMs before full CTAs
+    const size_t smem = (size_t)a.per_cta * half * sizeof(float2);
+    const dim3 grid(ceil_div(a.rows, a.per_cta));
+    if (a.g.interleaved)
+        CASS_PDL_LAUNCH((k_rope<T, V, true>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
+    else
+        CASS_PDL_LAUNCH((k_rope<T, V, false>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
+    return CASS_OK;
+}
+
+// 16-byte vectors where sizes, strides and places allow them, else words of two 16-bit values, else single values.
 template <class T>
-static int run_rope(const cass_rope_geom& g, const double* freqs, const int32_t* positions, int rows, const void* q, const void* k, void* q_out,
-                    void* k_out, int transpose, cudaStream_t s) {
-    constexpr int V = 16 / sizeof(T);
+static int choose_rope(const cass_rope_geom& g, const double* freqs, const int32_t* positions, int rows, const void* q, const void* k, void* q_out,
+                       void* k_out, int transpose, cudaStream_t s) {
     RopeArgs a{};
     a.g = g;
     a.rows = rows;
     a.transpose = transpose;
-    const int half = g.rot_dim / 2, heads = g.n_q_heads + g.n_k_heads;
     const bool in_place = (!q || q == q_out) && (!k || k == k_out);
     const int copied = in_place ? 0 : g.head_dim - g.rot_dim;            // values behind the pairs that have to move
     int64_t strides = 0;
     if (q) strides |= g.q_row | g.q_head | g.q_out_row | g.q_out_head;
     if (k) strides |= g.k_row | g.k_head | g.k_out_row | g.k_out_head;
     const uintptr_t at = (uintptr_t)q | (uintptr_t)k | (uintptr_t)q_out | (uintptr_t)k_out;
-    const bool wide = half % V == 0 && copied % (2 * V) == 0 && strides % V == 0 && at % 16 == 0;
-    const int v = wide ? V : 1;
-    a.rot_slots = half / v;
-    a.slots = a.rot_slots + ceil_div(copied, 2 * v);
-    a.per_cta = half >= kRopeThreads ? 1 : kRopeThreads / half;
-    if (a.per_cta > ceil_div(rows, kSms)) a.per_cta = ceil_div(rows, kSms);      // few rows: all SMs before full CTAs
-    while (a.per_cta > 1 && (int64_t)a.per_cta * heads > 4096) a.per_cta /= 2;
-    if ((int64_t)a.per_cta * heads > 65535) return CASS_ERR_UNSUPPORTED;
-    a.head_magic = heads == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)heads + 1u;         // u x heads < 2^32
-    const size_t smem = (size_t)a.per_cta * half * sizeof(float2);
-    const dim3 grid(ceil_div(rows, a.per_cta));
-    if (wide)
-        CASS_PDL_LAUNCH((k_rope<T, V>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
-    else
-        CASS_PDL_LAUNCH((k_rope<T, 1>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
-    return CASS_OK;
+    auto fits = [&](int v) { return g.rot_dim / 2 % v == 0 && copied % (2 * v) == 0 && strides % v == 0 && at % (v * sizeof(T)) == 0; };
+    constexpr int V = 16 / sizeof(T);
+    if (fits(V)) return run_rope<T, V>(a, freqs, positions, q, k, q_out, k_out, copied, s);
+    if constexpr (V == 8)
+        if (fits(2)) return run_rope<T, 2>(a, freqs, positions, q, k, q_out, k_out, copied, s);
+    return run_rope<T, 1>(a, freqs, positions, q, k, q_out, k_out, copied, s);
 }
 
 }  // namespace cass
@@ -252,7 +314,7 @@ extern "C" int cass_rope(const cass_rope_geom* geom, const double* freqs, const 
     if (k && k == k_out && ((rows > 1 && g.k_row != g.k_out_row) || (g.n_k_heads > 1 && g.k_head != g.k_out_head))) return CASS_ERR_INVALID_ARG;
     if (rows == 0) return CASS_OK;
     cudaStream_t s = (cudaStream_t)stream_;
-    if (g.dtype == CASS_BF16) return run_rope<__nv_bfloat16>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
-    if (g.dtype == CASS_F16) return run_rope<__half>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
-    return run_rope<float>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
+    if (g.dtype == CASS_BF16) return choose_rope<__nv_bfloat16>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
+    if (g.dtype == CASS_F16) return choose_rope<__half>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
+    return choose_rope<float>(g, freqs, positions, rows, q, k, q_out, k_out, transpose, s);
 }
