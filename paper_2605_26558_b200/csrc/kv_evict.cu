@@ -1,7 +1,9 @@
 // Eviction from a cache: of every (sequence, KV head) the first, the last and the heaviest positions stay and move to the front.
-// k_evict_select: the threshold by a radix selection of the weights' bits as ordered integers, eight bits a pass, then the
-// positions in order.  A cluster of CTAs takes a (sequence, head), each a contiguous part of the middle, read once and kept in shared
-// memory; histograms, then counts, cross the cluster through distributed shared memory.
+// k_evict_select: the threshold by a radix selection of the weights' bits as ordered integers, then the positions in order.  The range
+// that the weights take is cut into 2048 bins, the bin that the threshold falls into likewise, and so on: with bins of fixed bits a few were
+// hit by everybody, and additions to one address of shared memory queue (3.6 clocks each; 32 heads of 32768 positions 71 us).  Weights
+// without a bit set, which are many where a position got nothing, are counted by the warp.  A CTA takes a (sequence, head), its keys
+// read once and kept in registers; where they do not fit, a cluster does, and histograms and counts cross it through distributed shared memory.
 // k_evict_move: rows by 16-byte vectors.  Bound: memory (a kept row is read and written once), and for small caches the latency of the
 // selection's passes.
 #include <cooperative_groups.h>
@@ -12,37 +14,37 @@ namespace cg = cooperative_groups;
 
 namespace cass {
 
-constexpr int kEvThreads = 512;
+constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
-constexpr int kEvKeys = 40 * 1024;                       // most keys of a CTA that stay in shared memory
 constexpr int kEvMaxCluster = 8;
+constexpr uint32_t kEvZero = 0x80000000u;                // key of a weight of 0
 
 struct EvictArgs {
     int n_kv, capacity, budget, n_first, n_last;
 };
 
-// Larger weight, larger integer; -0 as +0, NaN below everything.
+// Larger weight, larger integer; -0 as +0, NaN 1, below every number; 0 is no key.
 __device__ __forceinline__ uint32_t weight_key(float w) {
-    const uint32_t u = __float_as_uint(w);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0u;
-    if (u == 0x80000000u) return 0x80000000u;
-    return (u >> 31) ? ~u : u | 0x80000000u;
+    const uint32_t u = __float_as_uint(w + 0.f);
+    const uint32_t k = u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
+    return w == w ? k : 1u;
 }
 
 struct EvictShared {
-    uint32_t hist[256 * 32];                             // a column a lane: the lanes of a warp never meet at an address
-    uint32_t bins[2][256];                               // this CTA's sums, read by the others; two, so that one barrier a pass is enough
+    uint32_t bins[2][2048];                              // this CTA's histogram, read by the others; two, so that one barrier a pass is enough
     uint32_t counts[2];                                  // positions above the threshold, at it
-    uint32_t total[256];
+    uint32_t warp_sum[kEvWarps];
     uint32_t warp_above[kEvWarps], warp_equal[kEvWarps];
-    uint32_t digit, left;
+    uint32_t warp_low[kEvWarps], warp_high[kEvWarps];
+    uint32_t range[3];                                   // of this CTA: the least and the largest key but zero's, zeros
+    uint32_t digit, left, all;
 };
 
-// grid: (CTAs of a cluster, KV heads, sequences)
-template <bool STAGED>
+// grid: (CTAs of a cluster, KV heads, sequences).  A warp takes a contiguous piece of its CTA's part, KEYS keys a lane; KEYS = 0: pieces of
+// any length, their weights read again in every pass.
+template <int KEYS>
 __global__ void __launch_bounds__(kEvThreads) k_evict_select(EvictArgs a, const float* __restrict__ weight, const int32_t* __restrict__ lens,
                                                              int32_t* __restrict__ kept_all) {
-    extern __shared__ uint32_t s_keys[];
     __shared__ EvictShared sh;
     cg::cluster_group cluster = cg::this_cluster();
     const int cs = (int)cluster.num_blocks(), rank = (int)cluster.block_rank();
@@ -57,101 +59,140 @@ __global__ void __launch_bounds__(kEvThreads) k_evict_select(EvictArgs a, const 
         for (int i = rank * kEvThreads + tid; i < a.budget; i += cs * kEvThreads) kept[i] = i < stay ? i : -1;
         return;
     }
+    const int mid = n - a.n_first - a.n_last, take = a.budget - a.n_first - a.n_last;      // take < mid
+    const int per = ceil_div(mid, cs), lo = min(rank * per, mid), m = min(per, mid - lo);  // this CTA's part of the middle
+    const int piece = KEYS ? KEYS * 32 : ceil_div(ceil_div(m, kEvWarps), 32) * 32, w0 = min(warp * piece, m), w1 = min(w0 + piece, m);
+    const float* w = weight + at * a.capacity + a.n_first + lo;
+    uint32_t keys[KEYS ? KEYS : 1];
+    if (KEYS && take) {
+#pragma unroll
+        for (int j = 0; j < KEYS; ++j) {
+            const int i = w0 + j * 32 + lane;
+            keys[j] = i < w1 ? weight_key(w[i]) : 0u;    // 0: no key
+        }
+    }
+    // every key of the warp's piece in order, 32 at a time: f(key or 0, position)
+    auto each = [&](auto f) {
+        if constexpr (KEYS > 0) {
+#pragma unroll
+            for (int j = 0; j < KEYS; ++j)
+                if (w0 + j * 32 < w1) f(keys[j], w0 + j * 32 + lane);
+        } else {
+            for (int i = w0; i < w1; i += 32) f(i + lane < w1 ? weight_key(w[i + lane]) : 0u, i + lane);
+        }
+    };
     for (int i = rank * kEvThreads + tid; i < a.n_first + a.n_last; i += cs * kEvThreads) {
         if (i < a.n_first) kept[i] = i;
         else kept[a.budget - a.n_last + (i - a.n_first)] = n - a.n_last + (i - a.n_first);
     }
-    const int mid = n - a.n_first - a.n_last, take = a.budget - a.n_first - a.n_last;      // take < mid
     if (take == 0) return;
-    const int per = ceil_div(mid, cs), lo = min(rank * per, mid), m = min(per, mid - lo);  // this CTA's part of the middle
-    const float* w = weight + at * a.capacity + a.n_first + lo;
-    if (STAGED)
-        for (int i = tid; i < m; i += kEvThreads) s_keys[i] = weight_key(w[i]);
-    auto key = [&](int i) { return STAGED ? s_keys[i] : weight_key(w[i]); };
-    uint32_t prefix = 0, left = (uint32_t)take;          // the threshold's bits so far; how many of the keys that share them stay
-#pragma unroll 1
-    for (int pass = 0; pass < 4; ++pass) {
-        const int shift = 24 - 8 * pass;
-        for (int i = tid; i < 256 * 32; i += kEvThreads) sh.hist[i] = 0;
-        __syncthreads();
-        for (int i = tid; i < m; i += kEvThreads) {
-            const uint32_t k = key(i);
-            if (pass == 0 || (k >> (shift + 8)) == prefix) atomicAdd(&sh.hist[((k >> shift) & 255u) * 32 + lane], 1u);
-        }
-        __syncthreads();
-        for (int b = warp; b < 256; b += kEvWarps) {
-            const uint32_t v = __reduce_add_sync(0xffffffffu, sh.hist[b * 32 + lane]);
-            if (lane == 0) sh.bins[pass & 1][b] = v;
-        }
+    // ---- the range of the keys other than zero's ----
+    uint32_t low = 0xFFFFFFFFu, high = 0u, zeros = 0u;
+    each([&](uint32_t k, int) {
+        if (k == kEvZero) ++zeros;
+        else { low = min(low, k - 1u); high = max(high, k); }          // (no key: the largest value, the least)
+    });
+    zeros = __reduce_add_sync(0xffffffffu, zeros);
+    low = __reduce_min_sync(0xffffffffu, low);
+    high = __reduce_max_sync(0xffffffffu, high);
+    if (lane == 0) { sh.warp_low[warp] = low; sh.warp_high[warp] = high; sh.warp_sum[warp] = zeros; }
+    __syncthreads();
+    low = __reduce_min_sync(0xffffffffu, sh.warp_low[lane]);
+    high = __reduce_max_sync(0xffffffffu, sh.warp_high[lane]);
+    zeros = __reduce_add_sync(0xffffffffu, sh.warp_sum[lane]);
+    if (cs > 1) {
+        if (tid == 0) { sh.range[0] = low; sh.range[1] = high; sh.range[2] = zeros; }
         cluster.sync();
-        if (tid < 256) {
-            uint32_t v = 0;
-            for (int c = 0; c < cs; ++c) v += cluster.map_shared_rank(&sh.bins[pass & 1][0], c)[tid];
-            sh.total[tid] = v;
+        const uint32_t* o = cluster.map_shared_rank(&sh.range[0], min(lane, cs - 1));
+        low = __reduce_min_sync(0xffffffffu, o[0]);
+        high = __reduce_max_sync(0xffffffffu, o[1]);
+        zeros = __reduce_add_sync(0xffffffffu, lane < cs ? o[2] : 0u);
+    }
+    ++low;                                               // 0 and no key: there are only zeros
+    const bool others = high != 0u, zero_in = others && kEvZero >= low && kEvZero <= high;
+    // ---- the threshold: the least key that stays, and how many of the keys at it ----
+    uint32_t threshold = kEvZero, left = (uint32_t)take, base = low, span = high - low;
+    int shift = others ? max(32 - __clz(span) - 11, 0) : 0;
+    bool search = others;
+    if (others && !zero_in && kEvZero > high) {          // zeros above all others
+        if (left <= zeros) search = false;
+        else left -= zeros;
+    }
+#pragma unroll 1
+    for (int pass = 0; search; ++pass) {
+        uint32_t* bins = sh.bins[pass & 1];
+        reinterpret_cast<uint2*>(bins)[tid] = make_uint2(0u, 0u);
+        __syncthreads();
+        each([&](uint32_t k, int) {
+            if (k - base <= span) atomicAdd(&bins[(k - base) >> shift], 1u);
+        });
+        if (cs > 1) cluster.sync();
+        else __syncthreads();
+        // two bins a thread, from the largest down
+        uint32_t v0 = 0, v1 = 0;
+        for (int c = 0; c < cs; ++c) {
+            const uint32_t* from = cs > 1 ? cluster.map_shared_rank(bins, c) : bins;
+            const uint2 x = reinterpret_cast<const uint2*>(from)[1023 - tid];
+            v0 += x.y;
+            v1 += x.x;
+        }
+        uint32_t upto = v0 + v1;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint32_t x = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += x;
+        }
+        if (lane == 31) sh.warp_sum[warp] = upto;
+        __syncthreads();
+        const uint32_t sums = sh.warp_sum[lane], before = upto - v0 - v1 + __reduce_add_sync(0xffffffffu, lane < warp ? sums : 0u);
+        if (pass == 0 && !zero_in && kEvZero < low) {    // zeros below all others
+            const uint32_t all = __reduce_add_sync(0xffffffffu, sums);
+            if (left > all) { left -= all; break; }
+        }
+        if (before < left && left <= before + v0 + v1) { // one thread: the count reaches `left` in one of its bins
+            const bool first = left <= before + v0;
+            sh.digit = 2047 - 2 * tid - (first ? 0 : 1);
+            sh.left = left - before - (first ? 0u : v0);
+            sh.all = sh.left == (first ? v0 : v1);
         }
         __syncthreads();
-        if (warp == 0) {
-            // bins from the largest down, eight a lane; the one in which the count reaches `left`
-            uint32_t v[8], sum = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) { v[i] = sh.total[255 - (lane * 8 + i)]; sum += v[i]; }
-            uint32_t before = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const uint32_t x = __shfl_up_sync(0xffffffffu, before, o);
-                if (lane >= o) before += x;
-            }
-            before -= sum;
-            if (before < left && left <= before + sum) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (before < left && left <= before + v[i]) { sh.digit = 255 - (lane * 8 + i); sh.left = left - before; }
-                    before += v[i];
-                }
-            }
-        }
-        __syncthreads();
-        prefix = (prefix << 8) | sh.digit;
+        base += sh.digit << shift;
         left = sh.left;
+        threshold = base;
+        if (sh.all || shift == 0) break;                 // the whole bin stays, from its lowest key on; or it has one key only
+        span = (1u << shift) - 1u;
+        shift = max(shift - 11, 0);
     }
-    // `prefix` is the threshold: all above it stay, and the first `left` at it.  A warp takes a contiguous piece of the part.
-    const int piece = ceil_div(ceil_div(m, kEvWarps), 32) * 32, w0 = min(warp * piece, m), w1 = min(w0 + piece, m);
+    // all above the threshold stay, and the first `left` at it
     uint32_t above = 0, equal = 0;
-    for (int i = w0; i < w1; i += 32) {
-        const bool in = i + lane < w1;
-        const uint32_t k = in ? key(i + lane) : 0u;
-        above += __popc(__ballot_sync(0xffffffffu, in && k > prefix));
-        equal += __popc(__ballot_sync(0xffffffffu, in && k == prefix));
-    }
+    each([&](uint32_t k, int) {
+        above += k > threshold;
+        equal += k == threshold;
+    });
+    above = __reduce_add_sync(0xffffffffu, above);
+    equal = __reduce_add_sync(0xffffffffu, equal);
     if (lane == 0) { sh.warp_above[warp] = above; sh.warp_equal[warp] = equal; }
     __syncthreads();
-    if (tid == 0) {
-        uint32_t x = 0, y = 0;
-        for (int i = 0; i < kEvWarps; ++i) { x += sh.warp_above[i]; y += sh.warp_equal[i]; }
-        sh.counts[0] = x;
-        sh.counts[1] = y;
+    // what lies before this warp: in its CTA, and in the CTAs before it
+    uint32_t a0 = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_above[lane] : 0u), e0 = __reduce_add_sync(0xffffffffu, lane < warp ? sh.warp_equal[lane] : 0u);
+    if (cs > 1) {
+        if (tid == kEvThreads - 1) { sh.counts[0] = a0 + above; sh.counts[1] = e0 + equal; }
+        cluster.sync();
+        const uint32_t* o = cluster.map_shared_rank(&sh.counts[0], min(lane, cs - 1));
+        a0 += __reduce_add_sync(0xffffffffu, lane < rank ? o[0] : 0u);
+        e0 += __reduce_add_sync(0xffffffffu, lane < rank ? o[1] : 0u);
     }
-    cluster.sync();
-    uint32_t a0 = 0, e0 = 0;                             // above and at the threshold before this warp's piece
-    for (int c = 0; c < rank; ++c) {
-        const uint32_t* o = cluster.map_shared_rank(&sh.counts[0], c);
-        a0 += o[0];
-        e0 += o[1];
-    }
-    for (int i = 0; i < warp; ++i) { a0 += sh.warp_above[i]; e0 += sh.warp_equal[i]; }
     const uint32_t lt = lanemask_lt();
     int32_t* out = kept + a.n_first;
-    for (int i = w0; i < w1; i += 32) {
-        const bool in = i + lane < w1;
-        const uint32_t k = in ? key(i + lane) : 0u;
-        const uint32_t ga = __ballot_sync(0xffffffffu, in && k > prefix), ge = __ballot_sync(0xffffffffu, in && k == prefix);
+    each([&](uint32_t k, int i) {
+        const uint32_t ga = __ballot_sync(0xffffffffu, k > threshold), ge = __ballot_sync(0xffffffffu, k == threshold);
+        if (!(ga | ge)) return;
         const uint32_t eq = e0 + __popc(ge & lt);        // ties before this position
-        const bool stay = in && (k > prefix || (k == prefix && eq < left));
-        if (stay) out[a0 + __popc(ga & lt) + min(eq, left)] = a.n_first + lo + i + lane;
+        if (k > threshold || (k == threshold && eq < left)) out[a0 + __popc(ga & lt) + min(eq, left)] = a.n_first + lo + i;
         a0 += __popc(ga);
         e0 += __popc(ge);
-    }
-    cluster.sync();                                      // nobody leaves while its counts may be read
+    });
+    if (cs > 1) cluster.sync();                          // nobody leaves while its counts may be read
 }
 
 // ---- moving what stays ----
@@ -250,24 +291,23 @@ bool cache_geom_ok(const cass_cache_geom& g, bool any) {
 }
 
 static int evict_cluster(const EvictArgs& a, int n_seq) {
-    int cs = 1;                                          // parts of at least 2048 positions, one CTA an SM
-    while (cs < kEvMaxCluster && a.capacity / (cs * 2) >= 2048 && (int64_t)n_seq * a.n_kv * cs * 2 <= kSms) cs *= 2;
-    while (cs < kEvMaxCluster && ceil_div(a.capacity, cs) > kEvKeys) cs *= 2;
+    int cs = 1;
+    while (cs < kEvMaxCluster && a.capacity / (cs * 2) >= 4 * kEvThreads && (int64_t)n_seq * a.n_kv * cs * 2 <= kSms) cs *= 2;
+    while (cs < kEvMaxCluster && ceil_div(a.capacity, cs) > kEvThreads * 16) cs *= 2;
     return cs;
 }
 
-template <bool STAGED>
-static int launch_select(const EvictArgs& a, int n_seq, int cs, size_t smem, const float* weight, const int32_t* lens, int32_t* kept, cudaStream_t s) {
-    CASS_ALLOW_SMEM(k_evict_select<STAGED>);
+template <int KEYS>
+static int launch_select(const EvictArgs& a, int n_seq, int cs, const float* weight, const int32_t* lens, int32_t* kept, cudaStream_t s) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(cs, a.n_kv, n_seq); cfg.blockDim = dim3(kEvThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
+    cfg.gridDim = dim3(cs, a.n_kv, n_seq); cfg.blockDim = dim3(kEvThreads); cfg.stream = s;
     cudaLaunchAttribute at[2];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = pdl_enabled();
     at[1].id = cudaLaunchAttributeClusterDimension;
     at[1].val.clusterDim.x = cs; at[1].val.clusterDim.y = 1; at[1].val.clusterDim.z = 1;
     cfg.attrs = at; cfg.numAttrs = 2;
-    if (cudaLaunchKernelEx(&cfg, k_evict_select<STAGED>, a, weight, lens, kept) != cudaSuccess) return CASS_ERR_CUDA;
+    if (cudaLaunchKernelEx(&cfg, k_evict_select<KEYS>, a, weight, lens, kept) != cudaSuccess) return CASS_ERR_CUDA;
     return CASS_OK;
 }
 
@@ -293,8 +333,12 @@ extern "C" int cass_kv_evict(const cass_cache_geom* cache, void* k_cache, void* 
     cudaStream_t s = (cudaStream_t)stream_;
     const EvictArgs a{g.n_kv_heads, g.capacity, budget, n_first, n_last};
     const int cs = evict_cluster(a, g.n_seq), per = ceil_div(g.capacity, cs);
-    const int rc = per <= kEvKeys ? launch_select<true>(a, g.n_seq, cs, (size_t)per * 4, weight, lens, kept, s)
-                                  : launch_select<false>(a, g.n_seq, cs, 0, weight, lens, kept, s);
+    const int rc = per <= kEvThreads       ? launch_select<1>(a, g.n_seq, cs, weight, lens, kept, s)
+                   : per <= 2 * kEvThreads  ? launch_select<2>(a, g.n_seq, cs, weight, lens, kept, s)
+                   : per <= 4 * kEvThreads  ? launch_select<4>(a, g.n_seq, cs, weight, lens, kept, s)
+                   : per <= 8 * kEvThreads  ? launch_select<8>(a, g.n_seq, cs, weight, lens, kept, s)
+                   : per <= 16 * kEvThreads ? launch_select<16>(a, g.n_seq, cs, weight, lens, kept, s)
+                                            : launch_select<0>(a, g.n_seq, cs, weight, lens, kept, s);
     if (rc) return rc;
     EvictMove m{};
     m.k = (const uint8_t*)k_cache; m.v = (const uint8_t*)v_cache; m.k_out = (uint8_t*)k_out; m.v_out = (uint8_t*)v_out;
