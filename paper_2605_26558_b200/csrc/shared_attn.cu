@@ -8,231 +8,186 @@
 namespace cass {
 
 // ---- joining the parts ----
-constexpr int kSmThreads = 256, kSmWarps = kSmThreads / 32;
-constexpr int kSmMaxParts = (2 * kSaLevels + 2) * kSms;          // of a pair: at most all units', and two of every CTA of the tensor-core kernel
-constexpr int kSmPos = 4 * kSmThreads;                   // positions of a weights block
 
-// Where the parts of (sequence b, head, pair p of the sequence) lie: those of the prefix, then those of its cache, in order.
+// Parts of one pair: at `o` and `ml`, `step` pairs apart.
 struct SaParts {
-    int64_t pre0, own0, pre_step;                        // first places, distance of two of the prefix (of the cache: a.pairs), in pairs
-    int n_pre, n_own;
-    bool pre_tc;
-    __device__ __forceinline__ int count() const { return n_pre + n_own; }
+    const float* o;
+    const float2* ml;
+    int64_t step;
+    int n;
 };
 
-__device__ SaParts shared_parts(const SharedAttn& a, const SaList& list, int seg_pairs, int b, int head, int p, int tiles_before, int n) {
-    SaParts r{};
-    const int all = b * a.rows * a.group + p;            // the pair among those of all sequences
-    if (list.p_tiles) {
-        const int s = all / seg_pairs * a.n_kv + head;
-        const int w0 = shared_unit_of(list, s * list.p_tiles), w1 = shared_unit_of(list, (s + 1) * list.p_tiles - 1);
-        r.pre0 = (int64_t)(w0 + s) * a.pairs + all % seg_pairs;
-        r.pre_step = a.pairs;
-        r.n_pre = w1 - w0 + 1;
-    } else if (a.prefix) {
-        const int cta = all / (2 * kStTile);
-        r.pre_tc = true;
-        if (cta < a.pre_n2) {
-            r.pre0 = ((int64_t)head * a.pre_n2 + cta) * 2 * kStTile + all % (2 * kStTile);
-            r.pre_step = (int64_t)a.n_kv * a.pre_n2 * 2 * kStTile;
-            r.n_pre = a.pre_s2;
-        } else {
-            r.pre0 = a.pre_at1 + (int64_t)head * kStTile + all % (2 * kStTile);
-            r.pre_step = (int64_t)a.n_kv * kStTile;
-            r.n_pre = 2 * a.pre_s1;
-        }
-    }
-    const int tiles = ceil_div(max(n, 0), kSaTok);
-    if (tiles) {
-        const int k = p / seg_pairs * a.n_kv + head, first = list.p_total + tiles_before * list.seq_segs + k * tiles;
-        const int w0 = shared_unit_of(list, first), w1 = shared_unit_of(list, first + tiles - 1);
-        r.own0 = (int64_t)(w0 + list.p_segs + b * list.seq_segs + k) * a.pairs + p % seg_pairs;
-        r.n_own = w1 - w0 + 1;
-    }
-    return r;
-}
+// grid: (query heads, rows, sequences), WARPS warps a head: one where there are many pairs, eight where there are few with many parts.
+// Bound: latency (two round trips behind the wait: where the parts lie, and the parts, eight of them together with a running maximum over
+// the rounds).  What runs once pays for each of its instructions, some 6 clocks: places by divisions in every block took 2 us more.
+constexpr int merge_threads(int warps) { return warps > 1 ? 32 * warps : 128; }
 
-// grid: blocks of the (sequence, row, query head)s, WARPS warps each, then (with weights) one for every 1024 positions of every (sequence, KV
-// head).  A warp a pair where there are many pairs, eight where there are few with many parts.
 template <int DT, int WARPS>
-__global__ void __launch_bounds__(kSmThreads) k_shared_merge(SharedAttn a, int seg_pairs, int pair_blocks, int pos_blocks, uint16_t* __restrict__ out,
-                                                             float* __restrict__ lse, const float* weight_in, float* weight_out,
-                                                             int32_t* __restrict__ d_status) {
+__global__ void __launch_bounds__(merge_threads(WARPS)) k_shared_merge(SharedAttn a, int seg_shift, uint32_t group_magic, uint16_t* __restrict__ out,
+                                                                       float* __restrict__ lse, int32_t* __restrict__ d_status) {
     using T = SaType<DT>;
-    __shared__ float s_w[WARPS == 1 ? kSmWarps : 1][kSmMaxParts];
-    __shared__ __align__(16) float s_o[WARPS == 1 ? 1 : kSmWarps][256];
+    constexpr int kWarps = merge_threads(WARPS) / 32, kParts = 8;
+    __shared__ __align__(16) float s_o[WARPS == 1 ? 1 : kWarps][256];
+    __shared__ float2 s_ml[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int P = a.rows * a.group;
-    const bool weights = (int)blockIdx.x >= pair_blocks;
-    int b, head, p = 0, r = 0, hq = 0, chunk = 0;
-    if (weights) {
-        int i = blockIdx.x - pair_blocks;
-        chunk = i % pos_blocks; i /= pos_blocks;
-        head = i % a.n_kv; b = i / a.n_kv;
-    } else {
-        const int i = blockIdx.x * (kSmWarps / WARPS) + warp / WARPS;
-        hq = i % a.n_q; r = i / a.n_q % a.rows; b = i / a.n_q / a.rows;
-        if (b >= a.n_seq) { pdl_wait(); return; }
-        head = hq / a.group; p = r * a.group + hq % a.group;
-    }
-    // The lengths were complete before the streaming kernel released this one: where the parts lie is known by the time they are there.
-    const int n = shared_len(a, b);
-    int before = 0, tiles = 0;
-    for (int i = lane; i < a.n_seq; i += 32) {
-        const int t = ceil_div(max(shared_len(a, i), 0), kSaTok);
-        tiles += t;
-        before += i < b ? t : 0;
-    }
-    before = __reduce_add_sync(0xffffffffu, before);
-    tiles = __reduce_add_sync(0xffffffffu, tiles);
-    const SaList list = shared_list(a, tiles);
-    const SaParts s = shared_parts(a, list, seg_pairs, b, head, p, before, n);
+    const int hq = blockIdx.x * (kWarps / WARPS) + warp / WARPS, r = blockIdx.y, b = blockIdx.z;
+    const int head = a.group == 1 ? hq : (int)__umulhi((uint32_t)hq, group_magic), P = a.rows * a.group, p = r * a.group + hq - head * a.group;
+    const int raw = a.lens ? a.lens[b] : 0, n = min(raw, a.capacity), seen = n - (a.rows - 1 - r);
     pdl_wait();
-    if (n < 0) return;                                   // the sequence is not there
-
-    // Maximum of all parts and their sum relative to it, by a warp; w: the parts' factors, 2^(m - M).  What 256 parts need is loaded in one go.
-    auto sums = [&](const SaParts& s, float* w, float& M, float& L) {
-        const int count = s.count();
-        const float *pm = s.pre_tc ? a.pre_m : a.part_m, *pl = s.pre_tc ? a.pre_l : a.part_l;
-        float m[8], l[8];
+    if (a.lse) pdl_launch_dependents();                  // the weights, behind
+    if (hq >= a.n_q || n < 0) return;                    // (n < 0: the sequence is not there)
+    if (p == 0 && head == 0 && warp % WARPS == 0 && lane == 0 && raw > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
+    // ---- where the parts lie: the prefix's, then the cache's ----
+    SaParts first, second;
+    const int all = b * P + p, seg = p >> seg_shift, in_seg = p & ((1 << seg_shift) - 1);        // the pair among those of all sequences; its segment
+    int2 pre = make_int2(0, -1), own = make_int2(0, -1);
+    if (a.p_groups) pre = a.slots[(all >> seg_shift) * a.n_kv + head];
+    if (n > 0) own = a.slots[a.p_groups * a.n_kv + (b * a.c_groups + seg) * a.n_kv + head];
+    if (a.prefix && !a.p_groups) {
+        const bool two = all / (2 * kStTile) < a.pre_n2;
+        const int64_t at = two ? ((int64_t)head * a.pre_n2 + all / (2 * kStTile)) * 2 * kStTile + all % (2 * kStTile)
+                               : a.pre_at1 + (int64_t)head * kStTile + all % (2 * kStTile);
+        first = {a.pre_o + at * a.d, a.pre_ml + at, (int64_t)a.n_kv * (two ? a.pre_n2 * 2 : 1) * kStTile, two ? a.pre_s2 : 2 * a.pre_s1};
+    } else {
+        const int64_t at = (int64_t)pre.x * a.pairs + (all & ((1 << seg_shift) - 1));
+        first = {a.part_o + at * a.d, a.part_ml + at, a.pairs, pre.y - pre.x + 1};
+    }
+    {
+        const int64_t at = (int64_t)own.x * a.pairs + in_seg;
+        second = {a.part_o + at * a.d, a.part_ml + at, a.pairs, own.y - own.x + 1};
+    }
+    const bool sees = a.prefix > 0 || seen > 0;
+    uint16_t* to = out + (int64_t)b * a.out_seq + (int64_t)r * a.out_row + (int64_t)hq * a.out_head;
+    auto put = [&](int c, float4 x, float L) {
+        const float inv = 1.f / L;
+        if (sees) *reinterpret_cast<uint2*>(to + c) = make_uint2(T::pack(x.x * inv, x.y * inv), T::pack(x.z * inv, x.w * inv));
+        else *reinterpret_cast<uint2*>(to + c) = make_uint2(0u, 0u);
+    };
+    float M = -INFINITY, L = 0.f;
+    for (int c = lane * 4; c < ((a.d + 127) & ~127); c += 128) {     // all lanes, also those beyond d
+        const bool in = c < a.d;
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
         M = -INFINITY;
         L = 0.f;
-        for (int i0 = lane; i0 - lane < count; i0 += 256) {
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+            const SaParts part = k ? second : first;
+            const int count = part.n;
+            const int64_t step = part.step * WARPS, step_o = step * a.d;
+            const float2* ml = part.ml + (warp % WARPS) * part.step;
+            const float* o = part.o + (warp % WARPS) * part.step * a.d + (in ? c : 0);
+#pragma unroll 1
+            for (int i = warp % WARPS; i < count; i += kParts * WARPS) {
+                // loads without a branch between them: the last part again where there are no more
+                float2 x[kParts];
+                float4 y[kParts];
+                float top = M;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int i = i0 + 32 * j;
-                m[j] = -INFINITY;
-                l[j] = 0.f;
-                if (i < count) {
-                    const bool pre = i < s.n_pre;
-                    const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * a.pairs;
-                    m[j] = (pre ? pm : a.part_m)[at];
-                    l[j] = (pre ? pl : a.part_l)[at];
+                for (int j = 0; j < kParts; ++j) {
+                    x[j] = *ml;
+                    y[j] = *reinterpret_cast<const float4*>(o);
+                    const bool more = i + (j + 1) * WARPS < count;
+                    ml += more ? step : 0;
+                    o += more ? step_o : 0;
                 }
-            }
-            float top = M;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, m[j]);
-            top = warp_max(top);
-            const float base = top == -INFINITY ? 0.f : top, fix = exp2_fast(M - base);
-            if (w && M != top)                           // beyond 256 parts: the factors so far follow
-                for (int i = lane; i < i0 - lane; i += 32) w[i] *= fix;
-            L *= fix;
-            M = top;
+                for (int j = 0; j < kParts; ++j) {
+                    if (j && i + j * WARPS >= count) { x[j] = make_float2(-INFINITY, 0.f); y[j] = make_float4(0.f, 0.f, 0.f, 0.f); }
+                    top = fmaxf(top, x[j].x);
+                }
+                const float base = top == -INFINITY ? 0.f : top, fix = exp2_fast(M - base);
+                M = top;
+                L *= fix;
+                sum.x *= fix; sum.y *= fix; sum.z *= fix; sum.w *= fix;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float f = exp2_fast(m[j] - base);
-                L += f * l[j];
-                if (w && i0 + 32 * j < count) w[i0 + 32 * j] = f;
-            }
-        }
-        L = warp_sum(L);
-        __syncwarp();
-    };
-    if (weights) {
-        const int pos = chunk * kSmPos + tid * 4, per_group = list.p_tiles ? seg_pairs : 2 * kStTile;
-        const float* in = weight_in ? weight_in + ((int64_t)b * a.n_kv + head) * a.capacity : nullptr;
-        float* to = weight_out + ((int64_t)b * a.n_kv + head) * a.capacity;
-        float* s_lse = &s_w[0][0];
-        float sum[4] = {0.f, 0.f, 0.f, 0.f}, was[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) was[i] = in && pos + i < a.capacity ? in[pos + i] : 0.f;
-        if (chunk * kSmPos < n) {
-            for (int q = warp; q < P; q += kSmWarps) {
-                SaParts t = s;                           // of pair 0: those of its neighbours lie beside them, up to the next group's
-                if (q / seg_pairs == 0 && (b * P + q) / per_group == b * P / per_group) { t.pre0 += q; t.own0 += q; }
-                else t = shared_parts(a, list, seg_pairs, b, head, q, before, n);
-                float M, L;
-                sums(t, nullptr, M, L);
-                if (lane == 0) s_lse[q] = M + log2f(L);
-            }
-            __syncthreads();
-            const float* from = a.scores + ((int64_t)b * a.n_kv + head) * P * a.score_stride + pos;
-            for (int q0 = 0; q0 < P; q0 += 8) {
-                float4 x[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (q0 + i < P && pos < n) x[i] = *reinterpret_cast<const float4*>(from + (q0 + i) * a.score_stride);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (q0 + i >= P) continue;
-                    const int end = n - (a.rows - 1 - (q0 + i) / a.group);           // what the pair sees
-                    const float z = s_lse[q0 + i], v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (pos + e < end) sum[e] += exp2_fast(v[e] - z);
+                for (int j = 0; j < kParts; ++j) {
+                    const float f = exp2_fast(x[j].x - base);
+                    L = fmaf(f, x[j].y, L);
+                    sum.x = fmaf(f, y[j].x, sum.x); sum.y = fmaf(f, y[j].y, sum.y); sum.z = fmaf(f, y[j].z, sum.z); sum.w = fmaf(f, y[j].w, sum.w);
                 }
             }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (pos + i < a.capacity && (pos + i < n || in != to)) to[pos + i] = was[i] + sum[i];
-        return;
-    }
-    if (p == 0 && head == 0 && warp % WARPS == 0 && lane == 0 && a.lens && a.lens[b] > a.capacity) atomicCAS(d_status, 0, CASS_ERR_CAPACITY);
-    const int parts = s.count();
-    float M, L, *w = s_w[WARPS == 1 ? warp : 0];
-    if (WARPS == 1 || warp == 0) sums(s, w, M, L);
-    if (WARPS > 1) {
-        __shared__ float s_total[2];
-        if (tid == 0) { s_total[0] = M; s_total[1] = L; }
-        __syncthreads();
-        M = s_total[0];
-        L = s_total[1];
-    }
-    const float* po = s.pre_tc ? a.pre_o : a.part_o;
-    const bool sees = a.prefix > 0 || n - (a.rows - 1 - r) > 0;
-    uint16_t* to = out + (int64_t)b * a.out_seq + (int64_t)r * a.out_row + (int64_t)hq * a.out_head;
-    auto put = [&](int c, float4 x) {
-        const uint32_t lo = T::put(sees ? x.x / L : 0.f) | ((uint32_t)T::put(sees ? x.y / L : 0.f) << 16);
-        const uint32_t hi = T::put(sees ? x.z / L : 0.f) | ((uint32_t)T::put(sees ? x.w / L : 0.f) << 16);
-        *reinterpret_cast<uint2*>(to + c) = make_uint2(lo, hi);
-    };
-    for (int c = lane * 4; c < a.d; c += 128) {
-        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int i0 = warp % WARPS; i0 < parts; i0 += 8 * WARPS) {               // eight parts under way
-            float4 x[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int i = i0 + j * WARPS;
-                if (i >= parts) continue;
-                const bool pre = i < s.n_pre;
-                const int64_t at = pre ? s.pre0 + i * s.pre_step : s.own0 + (int64_t)(i - s.n_pre) * a.pairs;
-                x[j] = *reinterpret_cast<const float4*>((pre ? po : a.part_o) + at * a.d + c);
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                if (i0 + j * WARPS >= parts) continue;
-                const float f = w[i0 + j * WARPS];
-                sum.x = fmaf(f, x[j].x, sum.x); sum.y = fmaf(f, x[j].y, sum.y); sum.z = fmaf(f, x[j].z, sum.z); sum.w = fmaf(f, x[j].w, sum.w);
-            }
-        }
-        if (WARPS == 1) put(c, sum);
-        else *reinterpret_cast<float4*>(&s_o[warp][c]) = sum;
+        if (WARPS == 1) { if (in) put(c, sum, L); }
+        else if (in) *reinterpret_cast<float4*>(&s_o[warp][c]) = sum;
     }
     if (WARPS > 1) {
+        if (lane == 0) s_ml[warp] = make_float2(M, L);
         __syncthreads();
-        if (warp == 0)
-            for (int c = lane * 4; c < a.d; c += 128) {
-                float4 x = *reinterpret_cast<const float4*>(&s_o[0][c]);
+        if (warp != 0) return;
+        const float2 x = lane < WARPS ? s_ml[lane] : make_float2(-INFINITY, 0.f);
+        M = warp_max(x.x);
+        const float f = exp2_fast(x.x - (M == -INFINITY ? 0.f : M));
+        L = warp_sum(f * x.y);
+        for (int c = lane * 4; c < ((a.d + 127) & ~127); c += 128) {
+            float4 z = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                for (int i = 1; i < WARPS; ++i) {
-                    const float4 y = *reinterpret_cast<const float4*>(&s_o[i][c]);
-                    x.x += y.x; x.y += y.y; x.z += y.z; x.w += y.w;
-                }
-                put(c, x);
+            for (int i = 0; i < WARPS; ++i) {
+                const float g = __shfl_sync(0xffffffffu, f, i);
+                const float4 y = *reinterpret_cast<const float4*>(&s_o[i][c < a.d ? c : 0]);
+                z.x = fmaf(g, y.x, z.x); z.y = fmaf(g, y.y, z.y); z.z = fmaf(g, y.z, z.z); z.w = fmaf(g, y.w, z.w);
             }
+            if (c < a.d) put(c, z, L);
+        }
     }
-    if (lse && warp % WARPS == 0 && lane == 0) lse[((int64_t)b * a.rows + r) * a.n_q + hq] = sees ? (M + log2f(L)) * 0.693147180559945309f : -INFINITY;
+    if (lane == 0) {
+        const float z = M + log2f(L);
+        if (lse) lse[((int64_t)b * a.rows + r) * a.n_q + hq] = sees ? z * 0.693147180559945309f : -INFINITY;
+        if (a.lse) a.lse[((int64_t)b * a.n_kv + head) * P + p] = z;
+    }
+}
+
+// The weights that the positions of the caches got: the scores' share of the sums.  grid: (blocks of 512 positions, KV heads, sequences).
+// The scores were there before the merge released this kernel; they travel while it finishes.
+constexpr int kSwThreads = 128, kSwPairs = 8, kSwMaxPairs = 256;
+
+__global__ void __launch_bounds__(kSwThreads) k_shared_weights(SharedAttn a, const float* in, float* out) {
+    __shared__ float s_lse[kSwMaxPairs];
+    __shared__ int s_end[kSwMaxPairs];
+    const int tid = threadIdx.x, head = blockIdx.y, b = blockIdx.z, P = a.rows * a.group;
+    const int n = shared_len(a, b), pos = (blockIdx.x * kSwThreads + tid) * 4;
+    const int64_t row = (int64_t)b * a.n_kv + head;
+    const float* from = a.scores + row * P * a.score_stride + min(pos, max(n - 1, 0) & ~3);
+    float4 x[kSwPairs];
+    auto load = [&](int q0) {
+#pragma unroll
+        for (int i = 0; i < kSwPairs; ++i) x[i] = *reinterpret_cast<const float4*>(from + (int64_t)min(q0 + i, P - 1) * a.score_stride);
+    };
+    if (n > 0) load(0);
+    pdl_wait();
+    if (n < 0) return;                                   // the sequence is not there
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n > 0) {
+        for (int q = tid; q < P; q += kSwThreads) {
+            s_lse[q] = a.lse[row * P + q];
+            s_end[q] = n - (a.rows - 1 - q / a.group);   // what the pair sees
+        }
+        __syncthreads();
+        for (int q0 = 0; q0 < P; q0 += kSwPairs) {
+            if (q0) load(q0);
+#pragma unroll
+            for (int i = 0; i < kSwPairs; ++i) {
+                if (q0 + i >= P) break;
+                const int left = s_end[q0 + i] - pos;
+                const float z = s_lse[q0 + i], v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sum[e] += e < left ? exp2_fast(v[e] - z) : 0.f;
+            }
+        }
+    }
+    in = in ? in + row * a.capacity : nullptr;
+    out += row * a.capacity;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (pos + i < a.capacity && (pos + i < n || in != out)) out[pos + i] = (in ? in[pos + i] : 0.f) + sum[i];
 }
 
 // ---- host ----
 
 struct SaPlan {
     SharedAttn a;
-    int mt, units;                                       // units: no list that there can be has more
+    int mt, levels;
     bool tc;
-    size_t at_o, at_m, at_l, at_scores, at_pre_o, at_pre_m, at_pre_l, bytes;
+    size_t at_o, at_ml, at_slots, at_scores, at_lse, at_pre_o, at_pre_ml, bytes;
 };
 
 constexpr int kSmManyPairs = 4 * kSms;                   // joined by a warp each
@@ -277,19 +232,20 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     const int64_t tiles = (int64_t)a.p_groups * a.n_kv * ceil_div(a.prefix, kSaTok) + (int64_t)a.n_seq * a.n_kv * a.c_groups * (a.capacity / kSaTok + 1);
     if (tiles > kSaMaxTiles) return CASS_ERR_UNSUPPORTED;
     a.ctas = kSms * shared_stream_per_sm(a.d, plan->mt);
-    plan->units = (int)(tiles < kSaLevels * a.ctas ? tiles : kSaLevels * a.ctas);
+    if (tiles < a.ctas) a.ctas = tiles > 1 ? (int)tiles : 1;
+    plan->levels = shared_levels((int)(tiles / a.ctas));
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o2 = off; off = align_up(off + b, 256); return o2; };
-    const size_t slots = (size_t)kSaLevels * a.ctas + (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups);
+    const size_t segments = (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups), slots = (size_t)kSaLevels * a.ctas + segments;
     plan->at_o = take(slots * a.pairs * a.d * 4);
-    plan->at_m = take(slots * a.pairs * 4);
-    plan->at_l = take(slots * a.pairs * 4);
+    plan->at_ml = take(slots * a.pairs * 8);
+    plan->at_slots = take(segments * 8);
     a.behind_tc = plan->tc;
     const size_t pre = plan->tc ? (size_t)shared_tc_plan(a) : 0;
     plan->at_pre_o = take(pre * a.d * 4);
-    plan->at_pre_m = take(pre * 4);
-    plan->at_pre_l = take(pre * 4);
+    plan->at_pre_ml = take(pre * 8);
     plan->at_scores = take(with_weights ? (size_t)a.n_seq * a.n_q * a.rows * a.score_stride * 4 : 0);
+    plan->at_lse = take(with_weights ? (size_t)a.n_seq * a.n_q * a.rows * 4 : 0);
     plan->bytes = off < 256 ? 256 : off;
     return CASS_OK;
 }
@@ -299,19 +255,17 @@ static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float
     const SharedAttn& a = plan.a;
     int rc = plan.tc ? launch_shared_prefix_tc(a, DT, d_status, s) : CASS_OK;
     if (rc) return rc;
-    rc = DT == CASS_BF16 ? launch_shared_stream_bf16(a, plan.mt, plan.units, d_status, s) : launch_shared_stream_f16(a, plan.mt, plan.units, d_status, s);
+    rc = DT == CASS_BF16 ? launch_shared_stream_bf16(a, plan.mt, plan.levels, d_status, s) : launch_shared_stream_f16(a, plan.mt, plan.levels, d_status, s);
     if (rc) return rc;
-    const int pos_blocks = weight_out ? ceil_div(a.capacity, kSmPos) : 0;
-    const int64_t pairs = (int64_t)a.n_seq * a.rows * a.n_q;
-    const bool many = pairs >= kSmManyPairs;
-    const int64_t pair_blocks = many ? (pairs + kSmWarps - 1) / kSmWarps : pairs, blocks = pair_blocks + (int64_t)a.n_seq * a.n_kv * pos_blocks;
-    if (blocks > 0x7FFFFFFF) return CASS_ERR_UNSUPPORTED;
-    if (many)
-        CASS_PDL_LAUNCH((k_shared_merge<DT, 1>), dim3((unsigned)blocks), dim3(kSmThreads), 0, s, a, 16 * plan.mt, (int)pair_blocks, pos_blocks, out, lse,
-                        weight_in, weight_out, d_status);
+    const uint32_t magic = a.group == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)a.group + 1u;         // head x group < 2^32
+    const int seg_shift = plan.mt == 1 ? 4 : plan.mt == 2 ? 5 : 6;
+    if ((int64_t)a.n_seq * a.rows * a.n_q >= kSmManyPairs)
+        CASS_PDL_LAUNCH((k_shared_merge<DT, 1>), dim3(ceil_div(a.n_q, merge_threads(1) / 32), a.rows, a.n_seq), dim3(merge_threads(1)), 0, s, a, seg_shift,
+                        magic, out, lse, d_status);
     else
-        CASS_PDL_LAUNCH((k_shared_merge<DT, kSmWarps>), dim3((unsigned)blocks), dim3(kSmThreads), 0, s, a, 16 * plan.mt, (int)pair_blocks, pos_blocks, out,
-                        lse, weight_in, weight_out, d_status);
+        CASS_PDL_LAUNCH((k_shared_merge<DT, 8>), dim3(a.n_q, a.rows, a.n_seq), dim3(merge_threads(8)), 0, s, a, seg_shift, magic, out, lse, d_status);
+    if (weight_out)
+        CASS_PDL_LAUNCH(k_shared_weights, dim3(ceil_div(a.capacity, kSwThreads * 4), a.n_kv, a.n_seq), dim3(kSwThreads), 0, s, a, weight_in, weight_out);
     return CASS_OK;
 }
 
@@ -343,9 +297,10 @@ extern "C" int cass_shared_prefix_attention(const cass_cache_geom* cache, const 
     uint8_t* mem = (uint8_t*)scratch;
     a.q = (const uint16_t*)q; a.kp = (const uint16_t*)k_prefix; a.vp = (const uint16_t*)v_prefix;
     a.kc = (const uint16_t*)k_cache; a.vc = (const uint16_t*)v_cache; a.lens = a.capacity ? lens : nullptr;
-    a.part_o = (float*)(mem + plan.at_o); a.part_m = (float*)(mem + plan.at_m); a.part_l = (float*)(mem + plan.at_l);
-    a.pre_o = (float*)(mem + plan.at_pre_o); a.pre_m = (float*)(mem + plan.at_pre_m); a.pre_l = (float*)(mem + plan.at_pre_l);
+    a.part_o = (float*)(mem + plan.at_o); a.part_ml = (float2*)(mem + plan.at_ml); a.slots = (int2*)(mem + plan.at_slots);
+    a.pre_o = (float*)(mem + plan.at_pre_o); a.pre_ml = (float2*)(mem + plan.at_pre_ml);
     a.scores = weight_out ? (float*)(mem + plan.at_scores) : nullptr;
+    a.lse = weight_out ? (float*)(mem + plan.at_lse) : nullptr;
     if (cache->dtype == CASS_BF16) return run_shared<CASS_BF16>(plan, (uint16_t*)out, lse, weight_in, weight_out, d_status, (cudaStream_t)stream_);
     return run_shared<CASS_F16>(plan, (uint16_t*)out, lse, weight_in, weight_out, d_status, (cudaStream_t)stream_);
 }

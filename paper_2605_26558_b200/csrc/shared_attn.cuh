@@ -54,17 +54,21 @@ struct SharedAttn {
     const uint16_t *q, *kp, *vp, *kc, *vc;
     const int32_t* lens;
     // scratch.  A part: the unnormalised output, maximum and sum of up to `pairs` (row, query head) pairs over some positions.
-    float *part_o, *part_m, *part_l;                     // [slot][pairs][d], [slot][pairs], [slot][pairs]
+    float* part_o;                                       // [slot][pairs][d]
+    float2* part_ml;                                     // [slot][pairs]
+    int2* slots;                                         // [segment]: the first and the last slot of the streaming kernel's parts
     float* scores;                                       // [sequence][KV head][pair][score_stride], for the weights; or null
     int64_t score_stride;                                // the capacity, rounded up to 4
+    float* lse;                                          // [sequence][KV head][pair], in powers of two, for the weights
     // the streaming kernel's work
     int behind_tc;                                       // it is launched behind the tensor-core kernel, whose parts it does not need
-    int ctas, pairs;                                     // CTAs that fit the GPU; pairs of a segment, at most
+    int ctas, pairs;                                     // spans at most (CTAs that fit the GPU, tiles that there can be); pairs of a segment, at most
     int p_groups, c_groups;                              // segments of pairs of the prefix (0: not this kernel's) and of a sequence
     // The prefix by the tensor-core kernel: the pairs of all sequences in tiles of 128.  Two tiles a CTA, `pre_n2` CTAs a head, its positions over
     // `pre_s2` CTAs: parts [split][head][CTA][256].  What is left over, one tile, over `pre_s1` (0: nothing is left): parts
     // [2 split + warpgroup][head][128], pre_at1 pairs further.
-    float *pre_o, *pre_m, *pre_l;
+    float* pre_o;
+    float2* pre_ml;
     int pre_n2, pre_s2, pre_s1;
     int64_t pre_at1;
 };
@@ -81,18 +85,17 @@ __device__ __forceinline__ int shared_len(const SharedAttn& a, int b) {
 }
 
 // The streaming kernel's segments are numbered: those of the prefix (group, head), then those of the sequences (sequence, group,
-// head); their tiles form one list of T, cut into units.  A CTA takes one unit after another, and a unit's part of segment s goes to slot
-// unit + s (from one part to the next either number grows, so no two share a slot).  SMs do not get the same share of the memory's
-// rate (of equal parts of one cache of 32000 positions the first ends 21 us after the start, the last 30), so the units shrink: the first
-// 3/4 of the list in as many units as CTAs fit the GPU, then 3/16 and 1/16 likewise, a tile at least.
+// head); their tiles form one list, cut into as many even spans as CTAs fit the GPU (a tile at least).  SMs do not get the same share of the
+// memory's rate (of equal spans of one cache of 32000 positions the first ends 21 us after the start, the last 30), so a span is cut again,
+// into 3/4, 3/16 and 1/16 of it where it has 16 tiles (3/4 and 1/4 where it has 4, not at all below), and the CTAs take first the large
+// pieces, then, as they get free, the small ones.  (Small pieces at the
+// list's end instead leave the last segment with hundreds of parts.)  Pieces are numbered along the list, and the part of piece u that lies
+// in segment s goes to slot u + s (from one part to the next either number grows, so no two share a slot).
 constexpr int kSaLevels = 3;
+__host__ __device__ inline int shared_levels(int each) { return each >= 16 ? 3 : each >= 4 ? 2 : 1; }         // pieces of a span, none of them empty
 struct SaList {
-    int p_tiles, p_total, seq_segs, p_segs, total, ctas;
-    int tile[kSaLevels + 1], unit[kSaLevels + 1];        // first tile and first unit of every level, and the end
+    int p_tiles, p_total, seq_segs, p_segs, total, spans, each, more, levels;
 };
-__host__ __device__ inline int shared_level_tile(int total, int level) {
-    return level == 0 ? 0 : level == 1 ? (int)((int64_t)total * 3 / 4) : level == 2 ? (int)((int64_t)total * 15 / 16) : total;
-}
 __device__ __forceinline__ SaList shared_list(const SharedAttn& a, int c_tiles) {      // c_tiles: tiles of all sequences' lengths
     SaList s;
     s.p_tiles = a.p_groups ? ceil_div(a.prefix, kSaTok) : 0;
@@ -100,44 +103,23 @@ __device__ __forceinline__ SaList shared_list(const SharedAttn& a, int c_tiles) 
     s.seq_segs = a.c_groups * a.n_kv;
     s.p_total = s.p_tiles * s.p_segs;
     s.total = s.p_total + c_tiles * s.seq_segs;
-    s.ctas = a.ctas;
-    s.tile[0] = s.unit[0] = 0;
-#pragma unroll
-    for (int i = 0; i < kSaLevels; ++i) {
-        s.tile[i + 1] = shared_level_tile(s.total, i + 1);
-        s.unit[i + 1] = s.unit[i] + min(s.tile[i + 1] - s.tile[i], a.ctas);
-    }
+    s.spans = max(min(s.total, a.ctas), 1);
+    s.each = s.total / s.spans;
+    s.more = s.total - s.each * s.spans;
+    s.levels = shared_levels(s.each);
     return s;
 }
-__device__ __forceinline__ int shared_first_tile(const SaList& s, int u) {             // of unit u, or the end
-    int t0 = s.tile[0], t1 = s.tile[1], u0 = s.unit[0], u1 = s.unit[1];
-#pragma unroll
-    for (int i = 1; i < kSaLevels; ++i)
-        if (u >= s.unit[i]) { t0 = s.tile[i]; t1 = s.tile[i + 1]; u0 = s.unit[i]; u1 = s.unit[i + 1]; }
-    if (u >= s.unit[kSaLevels]) return s.total;
-    const int w = u - u0;
-    if (u1 - u0 < s.ctas) return t0 + w;                 // a tile each
-    const int each = (t1 - t0) / s.ctas, more = t1 - t0 - each * s.ctas;
-    return t0 + w * each + w * more / s.ctas;            // w (t1 - t0) / ctas
-}
-__device__ __forceinline__ int shared_unit_of(const SaList& s, int t) {                 // that tile t is in
-    int t0 = s.tile[0], t1 = s.tile[1], u0 = s.unit[0], u1 = s.unit[1];
-#pragma unroll
-    for (int i = 1; i < kSaLevels; ++i)
-        if (t >= s.tile[i]) { t0 = s.tile[i]; t1 = s.tile[i + 1]; u0 = s.unit[i]; u1 = s.unit[i + 1]; }
-    const uint32_t n = (uint32_t)(u1 - u0), tiles = (uint32_t)(t1 - t0);
-    if (n == tiles) return u0 + (t - t0);
-    // the largest w with w tiles / n <= t - t0, rounded down: ((t - t0 + 1) n - 1) / tiles
-    const uint64_t x = (uint64_t)(uint32_t)(t - t0 + 1) * n - 1;
-    return u0 + (x >> 32 ? (int)(x / tiles) : (int)((uint32_t)x / tiles));
+__device__ __forceinline__ int shared_span(const SaList& s, int w) { return w >= s.spans ? s.total : w * s.each + w * s.more / s.spans; }      // w total / spans
+__device__ __forceinline__ int shared_cut(const SaList& s, int tiles, int level) {       // tiles of a span before its piece `level`
+    return level == 0 ? 0 : level >= s.levels ? tiles : level == 1 ? tiles - tiles / 4 : tiles - tiles / 16;
 }
 constexpr int64_t kSaMaxTiles = 1 << 30;
 
 // CTAs of the streaming kernel that an SM holds.
 constexpr int shared_stream_per_sm(int d, int mt) { return mt <= 2 && d <= 128 ? 2 : 1; }
-// mt: tiles of 16 pairs that a CTA takes at a time, 1, 2 or 4 (1 beyond head size 128)
-int launch_shared_stream_bf16(const SharedAttn& a, int mt, int units, int32_t* d_status, cudaStream_t s);
-int launch_shared_stream_f16(const SharedAttn& a, int mt, int units, int32_t* d_status, cudaStream_t s);
+// mt: tiles of 16 pairs that a CTA takes at a time, 1, 2 or 4 (1 beyond head size 128); levels: pieces of a span at most
+int launch_shared_stream_bf16(const SharedAttn& a, int mt, int levels, int32_t* d_status, cudaStream_t s);
+int launch_shared_stream_f16(const SharedAttn& a, int mt, int levels, int32_t* d_status, cudaStream_t s);
 int launch_shared_prefix_tc(const SharedAttn& a, int dtype, int32_t* d_status, cudaStream_t s);
 
 }  // namespace cass

@@ -318,7 +318,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
             const int all = first + (two ? wg * kStTile : 0) + row;
             const int64_t at = two ? (((int64_t)split * a.n_kv + head) * a.pre_n2 + cta) * 2 * kStTile + wg * kStTile + row
                                    : a.pre_at1 + ((int64_t)(2 * split + wg) * a.n_kv + head) * kStTile + row;
-            if (all < P) { a.pre_m[at] = m; a.pre_l[at] = l; }
+            if (all < P) a.pre_ml[at] = make_float2(m, l);
             // through the ring (every product that read it is done), so that a warp's stores are whole rows
             float4* box = reinterpret_cast<float4*>(sT) + (warp - 4) * 32 * (D / 4);
 #pragma unroll

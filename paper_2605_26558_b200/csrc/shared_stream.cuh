@@ -83,7 +83,7 @@ struct SaSegment {
     int index, head, first, seq, n;                      // number; KV head; first pair; sequence (-1: prefix); positions
     int begin, end;                                      // tiles of the list
 };
-// Tiles of one segment in one unit, as the fetching warp describes them to the others; tiles < 0: there are no more.
+// Tiles of one segment in one piece of the list, as the fetching warp describes them to the others; tiles < 0: there are no more.
 struct alignas(16) SaRun {
     int slot, head, first, seq, n, pos, tiles, pad;      // slot of the part; KV head; first pair; sequence; positions; first position
 };
@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
     extern __shared__ uint8_t smem_dyn[];
     __shared__ float2 s_ml[S::sets][S::pairs];
     __shared__ uint64_t full[S::stages], empty[S::stages], r_full[S::runs], r_empty[S::runs], answered;
-    __shared__ __align__(16) uint4 s_answer;             // which unit comes next
+    __shared__ __align__(16) uint4 s_answer;             // which piece comes next
     __shared__ SaRun s_run[S::runs];
     uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
     const int tid = threadIdx.x, lane = tid & 31, warp = __shfl_sync(0xffffffffu, tid >> 5, 0);
@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
             ++left;
             if (++stage == S::stages) { stage = 0; parity ^= 1; }
         };
-        auto tell = [&](int unit, int t, int tiles) {    // a run and its queries
+        auto tell = [&](int piece, int t, int tiles) {    // a run and its queries
             const int slot = runs % S::runs;
             wait(&r_empty[slot], ((uint32_t)(runs / S::runs) & 1u) ^ 1u);
             if (!ok) return;
@@ -232,15 +232,20 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                     }
             }
             if (lane == 0) {
-                s_run[slot] = {unit + cur.index, cur.head, cur.first, cur.seq, cur.n, (t - cur.begin) * kSaTok, tiles, 0};
+                if (tiles > 0 && t == cur.begin) a.slots[cur.index].x = piece + cur.index;
+                if (tiles > 0 && t + tiles == cur.end) a.slots[cur.index].y = piece + cur.index;
+                s_run[slot] = {piece + cur.index, cur.head, cur.first, cur.seq, cur.n, (t - cur.begin) * kSaTok, tiles, 0};
                 asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&r_full[slot])) : "memory");
             }
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[slot])) : "memory");
         };
-        for (int unit = blockIdx.x, units = 0; unit >= 0 && ok; ++units) {
-            const int t0 = shared_first_tile(list, unit), t1 = shared_first_tile(list, unit + 1);
+        // CTAs of the grid are pieces: the first of every span, then the second of every span, ...
+        for (int cta = blockIdx.x, ctas = 0; cta >= 0 && ok; ++ctas) {
+            const int level = cta / a.ctas, w = cta - level * a.ctas, piece = w * list.levels + level;
+            const int first = shared_span(list, w), tiles = shared_span(list, w + 1) - first;
+            const int t0 = first + shared_cut(list, tiles, level), t1 = level < list.levels ? first + shared_cut(list, tiles, level + 1) : t0;
             bool asked = false;
-            auto ask = [&]() {                           // for the next unit, while this one is fetched
+            auto ask = [&]() {                           // for the next piece, while this one is fetched
                 if (!asked && lane == 0) {
                     mbar_expect_tx(&answered, 16);
                     take_over(&s_answer, &answered);
@@ -250,15 +255,15 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
             if (t0 < t1) find(t0);
             for (int t = t0; t < t1 && ok;) {
                 if (t >= cur.end) next();
-                const int end = min(t1, cur.end), tiles = end - t;
+                const int end = min(t1, cur.end);
                 fetch(t);
-                if (ok) tell(unit, t, tiles);
+                if (ok) tell(piece, t, end - t);
                 ask();
                 for (++t; t < end && ok; ++t) fetch(t);
             }
             ask();
-            wait(&answered, (uint32_t)units & 1u);
-            unit = ok ? taken_over(&s_answer) : -1;
+            wait(&answered, (uint32_t)ctas & 1u);
+            cta = ok ? taken_over(&s_answer) : -1;
             fence_proxy_async();                         // the next answer comes behind this reading
             __syncwarp();
         }
@@ -502,10 +507,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                 }
                 if (p < P) *reinterpret_cast<float2*>(part + (int64_t)8 * h * D + k * 8) = x;
             }
-            if (set == 0 && p < P && (lane & 3) == 0) {
-                a.part_m[(int64_t)run.slot * a.pairs + p] = all[h];
-                a.part_l[(int64_t)run.slot * a.pairs + p] = sum[h];
-            }
+            if (set == 0 && p < P && (lane & 3) == 0) a.part_ml[(int64_t)run.slot * a.pairs + p] = make_float2(all[h], sum[h]);
         }
         fence_proxy_async();
         arrive(release);
@@ -528,25 +530,25 @@ inline int shared_cache_map(CUtensorMap* map, const uint16_t* at, int d, int pos
 }
 
 template <int DT, int D, int MT>
-int run_shared_stream(const SharedAttn& a, const CUtensorMap* maps, int units, int32_t* d_status, cudaStream_t s) {
+int run_shared_stream(const SharedAttn& a, const CUtensorMap* maps, int levels, int32_t* d_status, cudaStream_t s) {
     using S = SaShape<D, MT>;
     CASS_ALLOW_SMEM(k_shared_stream<DT, D, MT>);
-    CASS_PDL_LAUNCH((k_shared_stream<DT, D, MT>), dim3(units > 0 ? units : 1), dim3(S::threads), (size_t)S::smem, s, maps[0], maps[1], maps[2], maps[3], a, d_status);
+    CASS_PDL_LAUNCH((k_shared_stream<DT, D, MT>), dim3(levels * a.ctas), dim3(S::threads), (size_t)S::smem, s, maps[0], maps[1], maps[2], maps[3], a, d_status);
     return CASS_OK;
 }
 
 template <int DT, int D>
-int run_shared_stream_d(const SharedAttn& a, int mt, const CUtensorMap* maps, int units, int32_t* d_status, cudaStream_t s) {
-    if (mt == 1) return run_shared_stream<DT, D, 1>(a, maps, units, d_status, s);
+int run_shared_stream_d(const SharedAttn& a, int mt, const CUtensorMap* maps, int levels, int32_t* d_status, cudaStream_t s) {
+    if (mt == 1) return run_shared_stream<DT, D, 1>(a, maps, levels, d_status, s);
     if constexpr (D <= 128) {
-        if (mt == 2) return run_shared_stream<DT, D, 2>(a, maps, units, d_status, s);
-        if (mt == 4) return run_shared_stream<DT, D, 4>(a, maps, units, d_status, s);
+        if (mt == 2) return run_shared_stream<DT, D, 2>(a, maps, levels, d_status, s);
+        if (mt == 4) return run_shared_stream<DT, D, 4>(a, maps, levels, d_status, s);
     }
     return CASS_ERR_UNSUPPORTED;
 }
 
 template <int DT>
-int launch_shared_stream(const SharedAttn& a, int mt, int units, int32_t* d_status, cudaStream_t s) {
+int launch_shared_stream(const SharedAttn& a, int mt, int levels, int32_t* d_status, cudaStream_t s) {
     CUtensorMap maps[4] = {};
     int rc = CASS_OK;
     if (a.p_groups) {
@@ -559,12 +561,12 @@ int launch_shared_stream(const SharedAttn& a, int mt, int units, int32_t* d_stat
     }
     if (rc) return rc;
     switch (a.d) {
-        case 32: return run_shared_stream_d<DT, 32>(a, mt, maps, units, d_status, s);
-        case 64: return run_shared_stream_d<DT, 64>(a, mt, maps, units, d_status, s);
-        case 96: return run_shared_stream_d<DT, 96>(a, mt, maps, units, d_status, s);
-        case 128: return run_shared_stream_d<DT, 128>(a, mt, maps, units, d_status, s);
-        case 192: return run_shared_stream_d<DT, 192>(a, mt, maps, units, d_status, s);
-        case 256: return run_shared_stream_d<DT, 256>(a, mt, maps, units, d_status, s);
+        case 32: return run_shared_stream_d<DT, 32>(a, mt, maps, levels, d_status, s);
+        case 64: return run_shared_stream_d<DT, 64>(a, mt, maps, levels, d_status, s);
+        case 96: return run_shared_stream_d<DT, 96>(a, mt, maps, levels, d_status, s);
+        case 128: return run_shared_stream_d<DT, 128>(a, mt, maps, levels, d_status, s);
+        case 192: return run_shared_stream_d<DT, 192>(a, mt, maps, levels, d_status, s);
+        case 256: return run_shared_stream_d<DT, 256>(a, mt, maps, levels, d_status, s);
     }
     return CASS_ERR_UNSUPPORTED;
 }

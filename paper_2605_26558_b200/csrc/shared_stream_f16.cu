@@ -3,6 +3,6 @@
 
 namespace cass {
 
-int launch_shared_stream_f16(const SharedAttn& a, int mt, int units, int32_t* d_status, cudaStream_t s) { return launch_shared_stream<CASS_F16>(a, mt, units, d_status, s); }
+int launch_shared_stream_f16(const SharedAttn& a, int mt, int levels, int32_t* d_status, cudaStream_t s) { return launch_shared_stream<CASS_F16>(a, mt, levels, d_status, s); }
 
 }  // namespace cass
