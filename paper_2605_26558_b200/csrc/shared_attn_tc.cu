@@ -18,6 +18,7 @@ constexpr int kStThreads = 384;                          // warp 0: TMA; warp 1:
 constexpr int kStRegsLaunch = 168, kStRegsIssue = 56, kStRegsSoftmax = 224;          // a softmax thread holds its 128 scores of a tile
 static_assert(128 * kStRegsIssue + 256 * kStRegsSoftmax <= kStThreads * kStRegsLaunch, "the shares come from what the block was launched with");
 constexpr uint32_t kStS = 0, kStO = 256;                 // tensor memory: two score (and P) buffers, two outputs, 128 columns each
+constexpr int kStFewTiles = 4;                           // (tiles of pairs, of positions) an SM up to which SMs are left to the streaming kernel
 constexpr float kStGrowth = 8.f;                         // of a maximum, in powers of two, before what came before is rescaled
 
 template <int D>
@@ -359,16 +360,25 @@ int64_t shared_tc_plan(SharedAttn& a) {
     const bool odd = pair_tiles & 1;
     a.pre_n2 = pair_tiles / 2;
     // CTAs over the positions: the least time of the slower kind with at most one CTA an SM (if there are not more heads and pairs
-    // than that anyway).  A tile of positions takes two tiles of pairs 2 units, one tile 1.4 (its K and V come for half the work); an
-    // output to be left behind 3.
+    // than that anyway).  A tile of positions takes two tiles of pairs 2.1 us (the products, 1.2 PFLOP/s), one tile 1.3 (K and V at the
+    // memory's rate); an output to be left behind 3.
+    // SMs are left to the streaming kernel, which starts beside this one: the products do not need the memory's rate that the caches do.
+    // Their share is what that kernel's tiles take, 0.6 us each (1.5 with more than 16 pairs), if the caches are 3/4 full, half at most; and
+    // half where there is little to do, as each SM more saves less than the parts that it leaves cost.  64 sequences (40 heads) behind
+    // 32768 positions with caches of 1000: 100 -> 89 us on 96 SMs, 8 sequences (32 heads) behind 4000 with 600: 23.9 -> 22.1 on 72.
     a.pre_s2 = a.pre_n2 ? 1 : 0;
     a.pre_s1 = odd ? 1 : 0;
+    const double here = (double)tiles * a.n_kv * (a.pre_n2 * 2.1 + (odd ? 1.3 : 0.0));
+    const double there = 0.75 * (a.capacity / kSaTok + 1) * a.n_seq * a.n_kv * a.c_groups * (a.rows * a.group > 16 ? 1.5 : 0.6);
+    const bool little = (int64_t)tiles * a.n_kv * pair_tiles <= kStFewTiles * kSms;
+    const double share = !a.capacity ? 0.0 : little ? 0.5 : there / (here + there) < 0.5 ? there / (here + there) : 0.5;
+    const int sms = kSms - (int)(share * kSms);
     double best = 1e30;
     for (int s2 = a.pre_n2 ? 1 : 0; s2 <= (a.pre_n2 ? (tiles < kSms ? tiles : kSms) : 0); ++s2) {
-        const int room = kSms / a.n_kv - s2 * a.pre_n2;
+        const int room = sms / a.n_kv - s2 * a.pre_n2;
         if (odd ? room < 1 : room < 0) break;
         const int s1 = !odd ? 0 : room < tiles ? room : tiles;
-        const double t2 = s2 ? ceil_div(tiles, s2) * 2.0 + 3.0 : 0.0, t1 = s1 ? ceil_div(tiles, s1) * 1.4 + 3.0 : 0.0, t = t1 > t2 ? t1 : t2;
+        const double t2 = s2 ? ceil_div(tiles, s2) * 2.1 + 3.0 : 0.0, t1 = s1 ? ceil_div(tiles, s1) * 1.3 + 3.0 : 0.0, t = t1 > t2 ? t1 : t2;
         if (t < best) { best = t; a.pre_s2 = s2; a.pre_s1 = s1; }
     }
     a.pre_at1 = (int64_t)a.pre_s2 * a.n_kv * a.pre_n2 * 2 * kStTile;
