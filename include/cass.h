@@ -413,16 +413,17 @@ typedef struct cass_cache_geom {
  * the new rows' among them, row r sees the whole prefix and the first lens[b] - (rows - 1 - r) positions of its cache:
  *   s = scale q.k;  out = sum_j softmax(s)_j v_j;  lse = ln sum_j e^{s_j}  (-inf, and out 0, for a row that sees nothing)
  * What a row does not see does not reach its results, whatever its bits.  A sequence with lens[b] < 0 is not there: nothing
- * of it is read or written.  A length beyond the capacity is cut to it, and d_status receives CASS_ERR_CAPACITY.
+ * of it is written.  A length beyond the capacity is cut to it, and d_status receives CASS_ERR_CAPACITY.
  * weight_out (optional): fp32 [n_seq][n_kv_heads][capacity] = weight_in (NULL: 0) + the attention weights that each position of
  * the sequence's own cache got in this call, summed over rows and the group's query heads: what cass_kv_evict goes by.
  * weight_out = weight_in adds in place.
  * q, out: dtype of the cache, 16-byte aligned, strides multiples of 8.  lse (optional): fp32 [n_seq][rows][n_q_heads].
  * prefix_len = 0 (pointers NULL) or capacity = 0 (pointers and lens NULL: every row sees the prefix alone) leave a part out.
- * head_dim 32, 64, 96, 128, 192 or 256; at most 16 query heads a KV head; n_seq up to 4096; CASS_ERR_UNSUPPORTED otherwise.
+ * head_dim 32, 64, 96, 128, 192 or 256; at most 16 query heads a KV head and 1024 in all; n_seq up to 1024; CASS_ERR_UNSUPPORTED otherwise.
  * Probabilities are rounded to the cache's type for the second product, sums are 32 bits.  Results are the same bits
  * on every call with the same inputs and sizes.  scratch: device, 16-byte aligned, of cass_shared_prefix_scratch_bytes; two calls
- * that may overlap on the GPU need their own.  d_status (required): device int32, left alone if nothing went wrong. */
+ * that may overlap on the GPU need their own.  d_status (required): device int32, left alone if nothing
+ * went wrong (also CASS_ERR_TIMEOUT: a bounded device wait ran out, results are undefined). */
 typedef struct cass_shared_attn {
     int n_q_heads, rows;
     int64_t q_seq, q_row, q_head, out_seq, out_row, out_head;

@@ -6,6 +6,7 @@
 // on the way (a tensor without storage, as under vmap; a CUDA that does not come up) becomes a Python exception.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -56,6 +57,15 @@ bool device_address(PyObject* o, void** out) {
     return false;
 }
 
+// A tensor on another device than the current one, where the kernels would run.
+bool elsewhere(PyObject* o) {
+    if (!THPVariable_Check(o)) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.get_device() == c10::cuda::current_device()) return false;
+    PyErr_SetString(PyExc_ValueError, "tensor on another device than the current one");
+    return true;
+}
+
 bool stream_handle(PyObject* o, void** out) {
     static bool initialised = false;       // under the interpreter lock
     if (o == Py_None && initialised) {
@@ -99,14 +109,16 @@ bool argument(PyObject* o, T* out) {
     else return convert(o, out);
 }
 
-template <auto F>
+// HERE: tensors have to be on the current device.
+template <auto F, bool HERE = false>
 struct Entry;
-template <class... A, int (*F)(A...)>
-struct Entry<F> {
+template <class... A, int (*F)(A...), bool HERE>
+struct Entry<F, HERE> {
     static constexpr size_t N = sizeof...(A);      // the last parameter of every entry point here is the stream
     template <size_t... I>
     static PyObject* run(PyObject* const* args, std::index_sequence<I...>) {
         std::tuple<A...> v;
+        if (HERE && (elsewhere(args[I]) || ...)) return nullptr;
         if (!(argument<I + 1 == N>(args[I], &std::get<I>(v)) && ...)) return nullptr;
         int rc;
         Py_BEGIN_ALLOW_THREADS
@@ -159,11 +171,12 @@ PyObject* stream_address(PyObject*, PyObject* const* a, Py_ssize_t n) {
 }
 
 #define CASS_ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Entry<&NAME>::call)), METH_FASTCALL, nullptr}
+#define CASS_ENTRY_HERE(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&Entry<&NAME, true>::call)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {
     CASS_ENTRY(cass_draft_gemv), CASS_ENTRY(cass_draft_gemv_batch), CASS_ENTRY(cass_draft_gemv_static), CASS_ENTRY(cass_kv_append),
     CASS_ENTRY(cass_set_len), CASS_ENTRY(cass_draft_step), CASS_ENTRY(cass_verify), CASS_ENTRY(cass_draft_attention), CASS_ENTRY(cass_accept),
-    CASS_ENTRY(cass_accept_sampling), CASS_ENTRY(cass_softmax), CASS_ENTRY(cass_sample), CASS_ENTRY(cass_rope_freqs), CASS_ENTRY(cass_rope),
-    CASS_ENTRY(cass_shared_prefix_attention), CASS_ENTRY(cass_kv_evict),
+    CASS_ENTRY(cass_accept_sampling), CASS_ENTRY(cass_softmax), CASS_ENTRY(cass_sample), CASS_ENTRY_HERE(cass_rope_freqs), CASS_ENTRY_HERE(cass_rope),
+    CASS_ENTRY_HERE(cass_shared_prefix_attention), CASS_ENTRY_HERE(cass_kv_evict),
     {"cass_verify_gemm", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&verify_gemm)), METH_FASTCALL, nullptr},
     {"stream_address", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(&stream_address)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};

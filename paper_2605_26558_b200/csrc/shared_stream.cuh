@@ -97,7 +97,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
     constexpr int kCount = S::warps * 32;                // threads that compute
     extern __shared__ uint8_t smem_dyn[];
     __shared__ float2 s_ml[S::sets][S::pairs];
-    __shared__ uint64_t full[S::stages], empty[S::stages], r_full[S::runs], r_empty[S::runs], answered;
+    __shared__ uint64_t full[S::stages], empty[S::stages], r_full[S::runs], r_empty[S::runs], answered, meet[S::sets];
     __shared__ __align__(16) uint4 s_answer;             // which piece comes next
     __shared__ SaRun s_run[S::runs];
     uint8_t* smem = reinterpret_cast<uint8_t*>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
@@ -106,13 +106,14 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
         for (int i = 0; i < S::stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], S::warps); }
         for (int i = 0; i < S::runs; ++i) { mbar_init(&r_full[i], 33); mbar_init(&r_empty[i], S::warps); }
         mbar_init(&answered, 1);
+        for (int i = 0; i < S::sets; ++i) mbar_init(&meet[i], MT);
         fence_mbar_init();
         for (const CUtensorMap* map : {&map_kp, &map_vp, &map_kc, &map_vc}) asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
     }
     uint8_t* sQ0 = smem + S::stages * S::stage_bytes;
     // Behind the tensor-core kernel, which leaves this one's inputs alone and was not released before they were complete, it is waited for at the end.
     if (!a.behind_tc) pdl_wait();
-    pdl_launch_dependents();                             // the merge counts the list while this kernel runs
+    pdl_launch_dependents();                             // the merge, whose CTAs take the SMs as they get free
     __syncthreads();
 
     // Tiles go through the stages in turn.  A wait that runs out flags the status; the warp then goes on without waiting, so that
@@ -215,7 +216,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
             if (tiles > 0) {
                 const int P = (cur.seq < 0 ? a.n_seq : 1) * a.rows * a.group;
                 uint8_t* to = sQ0 + slot * S::q_bytes;
-                int64_t row[kQRows];   // where the queries of a lane's pairs lie
+                int64_t row[kQRows];                     // where the queries of a lane's pairs lie
 #pragma unroll
                 for (int i = 0; i < kQRows; ++i) {
                     const int all = cur.first + lane + 32 * i, r = all / a.group, seq = cur.seq < 0 ? r / a.rows : cur.seq;
@@ -399,8 +400,8 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                     l[e >> 1] += s[j][e];
                 }
             // Positions that some of the sequence's rows do not see: what is no number in their V must not meet a 0 of P in the product.  It
-            // is added here, for the rows that see it, and taken out.  (In the product itself, guarded, the code was too long for the
-            // instruction cache: a quarter of the time.)
+            // is added here, for the rows that see it, and taken out.  (In the product's loop the guard took the loads ahead of the products
+            // apart, and made the code too long for the instruction cache: 16 x 5 rows behind 16000 positions 77 us for 63.)
             if (run.seq >= 0 && a.rows > 1 && pos0 + S::tok > run.n - (a.rows - 1) && pos0 < run.n) {
                 const int t_lo = max(run.n - (a.rows - 1) - pos0, 0), t_hi = min(run.n - pos0, S::tok);      // of this warp's positions
                 uint8_t* v = at + S::kv_bytes;
@@ -411,7 +412,17 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
 #pragma unroll
                     for (int c = 0; c < 4; ++c) odd |= (e[c] & T::kExponent) == T::kExponent || (e[c] >> 16 & T::kExponent) == T::kExponent;
                 }
-                if (__any_sync(0xffffffffu, odd)) {      // the same for all warps of these positions
+                // (The warps of these positions find the same.  They meet at a barrier with a bounded wait: after a wait that ran out they
+                // may have read different things.)
+                auto sync_set = [&](uint32_t parity) {       // two of them each time: phases 0 and 1
+                    __syncwarp();
+                    if (MT > 1) {
+                        if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&meet[set])) : "memory");
+                        mbar_wait_bounded(&meet[set], parity);
+                        __syncwarp();
+                    }
+                };
+                if (__any_sync(0xffffffffu, odd)) {
 #pragma unroll 1
                     for (int t = t_lo; t < t_hi; ++t) {
                         float x[2];                      // p of this thread's rows: in lane 4 row + (t % 8) / 2
@@ -435,7 +446,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                             }
                         }
                     }
-                    asm volatile("bar.sync %0, %1;" ::"r"(2 + set), "n"(MT * 32) : "memory");
+                    sync_set(0);
                     for (int j = t_lo * (D / 2) + lane; j < t_hi * (D / 2); j += 32) {
                         const int t = j / (D / 2), c = j % (D / 2);
                         uint32_t* w = reinterpret_cast<uint32_t*>(v + sa_at<D, kSaTok>(set * S::tok + t, c / 4) + (c % 4) * 4);
@@ -444,7 +455,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                         if ((bits >> 16 & T::kExponent) == T::kExponent) bits &= 0x0000FFFFu;
                         *w = bits;
                     }
-                    asm volatile("bar.sync %0, %1;" ::"r"(2 + set), "n"(MT * 32) : "memory");
+                    sync_set(1);
                     fence_proxy_async();                 // the next copy into the stage comes behind these writes
                 }
             }

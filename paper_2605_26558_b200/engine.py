@@ -81,6 +81,10 @@ class Engine:
         B.cass_session_reset(self.session)
         self.n_prompt = 0
 
+    def set_rope(self, params: B.RopeParams):
+        """Rotary positions scaled for longer contexts (see cass_rope_params); before the first prefill, or after reset()."""
+        B.cass_session_set_rope(self.session, params)
+
     def prefill(self, prompt: torch.Tensor, calibrate: bool = False):
         """Target pass over the prompt(s) ([n] or [batch][n] token ids, equal lengths; bf16 cache only); returns the first
         generated token (per sequence).  With calibrate, the Wanda activation statistics are accumulated on the way."""

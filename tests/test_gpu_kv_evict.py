@@ -129,6 +129,12 @@ def test_weights_that_are_hard_to_order(cass):
         check(cass, k, v, w.clone(), lens.clone(), budget, first, last)
 
 
+def test_a_budget_beyond_the_first_cache(cass):
+    """Into a larger cache: everything stays."""
+    k, v, w = make(3, 60, 2, 64)
+    check(cass, k, v, w, torch.tensor([60, 0, 59], dtype=torch.int32, device="cuda"), 80, 2, 4, out_cap=90)
+
+
 def test_lengths_that_mean_nothing_leave_a_sequence_alone(cass):
     k, v, w = make(5, 60, 2, 64)
     lens = torch.tensor([61, -1, 60, 0, 2 ** 31 - 1], dtype=torch.int32, device="cuda")

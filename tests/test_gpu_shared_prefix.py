@@ -181,6 +181,33 @@ def test_infinite_scores(cass, b):
     assert out[:, 0, :4][neg].isfinite().all() and out[:, 0, :4][~neg].isnan().all()
 
 
+def test_nothing_to_see(cass):
+    """No prefix and no cache: outputs 0, log sums -inf."""
+    c = Case(3, 2, 8, 2, 64, 0, 0, [0, 0, 0])
+    out, lse, _, status = c.run(cass, weights=False)
+    assert (out == 0).all() and (lse == -math.inf).all() and int(status.item()) == 0
+
+
+@pytest.mark.parametrize("nq,nk,d,rows,cap", [(40, 8, 128, 5, 700), (16, 1, 64, 16, 300), (32, 2, 128, 3, 200), (12, 4, 256, 7, 150)])
+def test_many_rows_of_a_sequence(cass, nq, nk, d, rows, cap):
+    """More pairs of a sequence and head than one, two or four tiles of 16 hold."""
+    Case(3, rows, nq, nk, d, 130, cap, [cap, rows, cap // 2], torch.float16, seed=rows).check(cass)
+
+
+@pytest.mark.parametrize("d", [64, 128, 96])
+@pytest.mark.parametrize("nq,nk,rows", [(16, 2, 5), (16, 1, 4), (4, 2, 2)])
+def test_values_that_are_no_numbers_behind_several_tiles_of_pairs(cass, d, nq, nk, rows):
+    c, clean = (Case(2, rows, nq, nk, d, 40, 200, [200, 67], seed=d) for _ in range(2))
+    for i, n in enumerate(c.lens):
+        c.vc[i, n - 1, :, 3::7], clean.vc[i, n - 1] = math.nan, 0
+    out, lse, _, _ = c.run(cass)
+    want, want_lse, _, _ = clean.run(cass)
+    assert torch.equal(out[:, :-1], want[:, :-1]) and torch.equal(lse, want_lse)
+    bad = torch.zeros(d, dtype=torch.bool, device="cuda")
+    bad[3::7] = True
+    assert out[:, -1][..., bad].isnan().all() and out[:, -1][..., ~bad].isfinite().all()
+
+
 def test_lengths_beyond_the_capacity_are_cut(cass):
     Case(3, 2, 8, 2, 64, 20, 50, [51, 50, 2 ** 31 - 1]).check(cass)
 
