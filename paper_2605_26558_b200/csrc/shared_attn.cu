@@ -17,7 +17,7 @@ struct SaParts {
     int n;
 };
 
-// grid: (query heads, rows, sequences), WARPS warps a head: one where there are many pairs, eight where there are few with many parts.
+// grid: (query heads, rows, sequences), WARPS warps a head: one where there are many pairs, more where there are few with many parts.
 // Bound: latency (two round trips behind the wait: where the parts lie, and the parts, eight of them together with a running maximum over
 // the rounds).  What runs once pays for each of its instructions, some 6 clocks: places by divisions in every block took 2 us more.
 constexpr int merge_threads(int warps) { return warps > 1 ? 32 * warps : 128; }
@@ -191,6 +191,7 @@ struct SaPlan {
 };
 
 constexpr int kSmManyPairs = 4 * kSms;                   // joined by a warp each
+constexpr int kSmFewPairs = kSms / 2;                    // joined by 16 warps where a list is long: one cache of 32000 positions 37.8 -> 36.5 us; 256 pairs 20.3 -> 22.9
 constexpr int kSaStreamPairs = 16;                       // pairs behind a prefix up to which it is streamed
 
 static bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
@@ -259,11 +260,14 @@ static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float
     if (rc) return rc;
     const uint32_t magic = a.group == 1 ? 0u : 0xFFFFFFFFu / (uint32_t)a.group + 1u;         // head x group < 2^32
     const int seg_shift = plan.mt == 1 ? 4 : plan.mt == 2 ? 5 : 6;
-    if ((int64_t)a.n_seq * a.rows * a.n_q >= kSmManyPairs)
-        CASS_PDL_LAUNCH((k_shared_merge<DT, 1>), dim3(ceil_div(a.n_q, merge_threads(1) / 32), a.rows, a.n_seq), dim3(merge_threads(1)), 0, s, a, seg_shift,
-                        magic, out, lse, d_status);
-    else
-        CASS_PDL_LAUNCH((k_shared_merge<DT, 8>), dim3(a.n_q, a.rows, a.n_seq), dim3(merge_threads(8)), 0, s, a, seg_shift, magic, out, lse, d_status);
+    const int64_t pairs = (int64_t)a.n_seq * a.rows * a.n_q;
+#define CASS_SHARED_MERGE(W_)                                                                                                               \
+    CASS_PDL_LAUNCH((k_shared_merge<DT, W_>), dim3(W_ > 1 ? a.n_q : ceil_div(a.n_q, merge_threads(1) / 32), a.rows, a.n_seq),                 \
+                    dim3(merge_threads(W_)), 0, s, a, seg_shift, magic, out, lse, d_status)
+    if (pairs >= kSmManyPairs) CASS_SHARED_MERGE(1);
+    else if (pairs <= kSmFewPairs && plan.levels > 1) CASS_SHARED_MERGE(16);
+    else CASS_SHARED_MERGE(8);
+#undef CASS_SHARED_MERGE
     if (weight_out)
         CASS_PDL_LAUNCH(k_shared_weights, dim3(ceil_div(a.capacity, kSwThreads * 4), a.n_kv, a.n_seq), dim3(kSwThreads), 0, s, a, weight_in, weight_out);
     return CASS_OK;

@@ -92,7 +92,7 @@ __device__ __forceinline__ int shared_len(const SharedAttn& a, int b) {
 // list's end instead leave the last segment with hundreds of parts.)  Pieces are numbered along the list, and the part of piece u that lies
 // in segment s goes to slot u + s (from one part to the next either number grows, so no two share a slot).
 constexpr int kSaLevels = 3;
-__host__ __device__ inline int shared_levels(int each) { return each >= 16 ? 3 : each >= 4 ? 2 : 1; }         // pieces of a span, none of them empty
+__host__ __device__ inline int shared_levels(int each) { return each >= 8 ? 3 : each >= 4 ? 2 : 1; }         // pieces of a span, none of them empty
 struct SaList {
     int p_tiles, p_total, seq_segs, p_segs, total, spans, each, more, levels;
 };
@@ -111,7 +111,7 @@ __device__ __forceinline__ SaList shared_list(const SharedAttn& a, int c_tiles) 
 }
 __device__ __forceinline__ int shared_span(const SaList& s, int w) { return w >= s.spans ? s.total : w * s.each + w * s.more / s.spans; }      // w total / spans
 __device__ __forceinline__ int shared_cut(const SaList& s, int tiles, int level) {       // tiles of a span before its piece `level`
-    return level == 0 ? 0 : level >= s.levels ? tiles : level == 1 ? tiles - tiles / 4 : tiles - tiles / 16;
+    return level == 0 ? 0 : level >= s.levels ? tiles : level == 1 ? tiles - tiles / 4 : tiles - max(tiles / 16, 1);
 }
 constexpr int64_t kSaMaxTiles = 1 << 30;
 
