@@ -192,7 +192,11 @@ struct SaPlan {
 
 constexpr int kSmManyPairs = 4 * kSms;                   // joined by a warp each
 constexpr int kSmFewPairs = kSms / 2;                    // joined by 16 warps where a list is long: one cache of 32000 positions 37.8 -> 36.5 us; 256 pairs 20.3 -> 22.9
-constexpr int kSaStreamPairs = 16;                       // pairs behind a prefix up to which it is streamed
+// A prefix is streamed behind up to 32 pairs a KV head while (pairs, 16 at least) x positions x KV heads is below this: a launch less.
+// us, streamed and on the tensor cores, 8 KV heads of 128: 4 pairs, 4000 positions 12.5, 14.1; 32000 positions 35.0, 30.6; 16 pairs 13.5, 15.2
+// and 40.0, 37.1; 24 pairs 15.9, 15.6 and 51.6, 37.8; 32 pairs, 1000 positions 16.1, 16.6; 2 heads of 64, 32 pairs, 2000 positions 9.4, 11.3.
+constexpr int kSaStreamPairs = 32;
+constexpr int64_t kSaStreamWork = 768 * 1024;
 
 static bool head_dim_ok(int d) { return d == 32 || d == 64 || d == 96 || d == 128 || d == 192 || d == 256; }
 
@@ -221,7 +225,7 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     a.c_seq = c->seq_stride; a.c_pos = c->pos_stride; a.c_head = c->head_stride;
     a.scale_log2 = (t->scale > 0.f ? t->scale : 1.0f / sqrtf((float)a.d)) * 1.44269504088896341f;
     const int P = a.rows * group, all = a.n_seq * P;     // pairs of a sequence, of all
-    plan->tc = a.prefix && all > kSaStreamPairs && shared_tc_usable(a);
+    plan->tc = a.prefix && shared_tc_usable(a) && (all > kSaStreamPairs || (int64_t)(all > 16 ? all : 16) * a.prefix * a.n_kv > kSaStreamWork);
     const int most = a.prefix && !plan->tc ? (all > P ? all : P) : P;
     plan->mt = a.d > 128 || most <= 16 ? 1 : most <= 32 ? 2 : 4;
     const int seg = 16 * plan->mt;
