@@ -3,9 +3,10 @@
 // that the weights take is cut into 2048 bins, the bin that the threshold falls into likewise, and so on: with bins of fixed bits a few were
 // hit by everybody, and additions to one address of shared memory queue (3.6 clocks each; 32 heads of 32768 positions 71 us).  Weights
 // without a bit set, which are many where a position got nothing, are counted by the warp.  A CTA takes a (sequence, head), its keys
-// read once and kept in registers; where they do not fit, a cluster does, and histograms and counts cross it through distributed shared memory.
-// k_evict_move: rows by 16-byte vectors.  Bound: memory (a kept row is read and written once), and for small caches the latency of the
-// selection's passes.
+// read once and kept in registers; long caches take a cluster, and histograms and counts cross it through distributed shared memory.
+// k_evict_move: rows by 16-byte vectors.
+// Bound: the selection's latency (its passes, each a few barriers) and, for the rows, memory (a kept row is read and written once).
+// 2 heads of 1152 positions 5.1 us of selection, 64 of 4095 7.2, 32 of 32768 15; the rows of the last (4096 kept of each, 67 MB in and out) 20 us.
 #include <cooperative_groups.h>
 
 #include "kernels.cuh"
@@ -290,6 +291,9 @@ bool cache_geom_ok(const cass_cache_geom& g, bool any) {
     return true;
 }
 
+// CTAs of a cluster.  Two or more where each still has 4096 positions or more (below that the cluster's barriers cost more than the
+// keys that a CTA has less: 64 heads of 4095 positions by pairs of CTAs 32.1 us, by one each 30.7) and every CTA has an SM; more where the
+// keys would not fit the registers (32 heads of 32768 by four CTAs of 8 keys a thread 37.0 us, by one of 32 74).
 static int evict_cluster(const EvictArgs& a, int n_seq) {
     int cs = 1;
     while (cs < kEvMaxCluster && a.capacity / (cs * 2) >= 4 * kEvThreads && (int64_t)n_seq * a.n_kv * cs * 2 <= kSms) cs *= 2;
@@ -350,7 +354,8 @@ extern "C" int cass_kv_evict(const cass_cache_geom* cache, void* k_cache, void* 
     m.cols = vecs;
     m.rows = budget;
     if (in_place) {
-        // all rows of a column range by one CTA: narrow ranges, down to a sector of 32 bytes, until every SM has one
+        // all rows of a column range by one CTA: narrow ranges, down to a sector of 32 bytes, until every SM has one.  8 heads of 128 dims,
+        // 2048 of 4096 positions kept: 25.6 us by whole rows, 10.4 so; four sequences of them 25.9 and 20.6; 8192 of 32768 kept: 89 and 41
         while (m.cols % 2 == 0 && m.cols > 2 && (int64_t)g.n_seq * g.n_kv_heads * 2 * (vecs / m.cols) < kSms) m.cols /= 2;
     } else {
         m.rows = kEvMoveThreads / m.cols * kEvMoveUnroll;

@@ -1,5 +1,5 @@
-// The streaming kernel of the shared-prefix attention: a prefix behind up to 64 (sequence, row, query head) pairs, and every sequence's own
-// cache.  Tiles of 64 positions come by TMA into a ring (one warp fetches, the others compute), both products run by mma.sync (16 pairs by
+// The streaming kernel of the shared-prefix attention: a prefix behind few (sequence, row, query head) pairs, or of a head size that the
+// tensor-core kernel does not take, and every sequence's own cache.  Tiles of 64 positions come by TMA into a ring (one warp fetches, the others compute), both products run by mma.sync (16 pairs by
 // 8 positions or dims), the softmax in registers with a running maximum.  What is bound by memory runs here: with few pairs a
 // position's bytes cost more time on the bus than in the products.  The positions of all segments form one list of tiles that the CTAs share,
 // whatever the lengths are, and the lengths are read on the device.
