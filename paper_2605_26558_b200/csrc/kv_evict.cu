@@ -161,7 +161,7 @@ __global__ void __launch_bounds__(kEvThreads) k_evict_select(EvictArgs a, const 
         left = sh.left;
         threshold = base;
         if (sh.all || shift == 0) break;                 // the whole bin stays, from its lowest key on; or it has one key only
-        span = (1u << shift) - 1u;
+        span = min((1u << shift) - 1u, high - base);     // (zeros may lie right behind the largest key, in its bin)
         shift = max(shift - 11, 0);
     }
     // all above the threshold stay, and the first `left` at it

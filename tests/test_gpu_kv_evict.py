@@ -129,6 +129,19 @@ def test_weights_that_are_hard_to_order(cass):
         check(cass, k, v, w.clone(), lens.clone(), budget, first, last)
 
 
+def test_zeros_right_behind_the_largest_weights(cass):
+    """Negative weights down to the smallest number and some zeros: the zeros stay, and so do the weights next to them."""
+    for cap, near, zeros in ((500, 7, 3), (3000, 60, 40), (9000, 300, 5), (20000, 2, 1)):
+        k, v, w = make(1, cap, 2, 64, seed=cap)
+        w = -(1 + w)
+        g = torch.Generator(device="cuda").manual_seed(cap)
+        at = torch.randperm(cap, generator=g, device="cuda")
+        w[:, :, at[:near]] = -torch.arange(1, near + 1, device="cuda", dtype=torch.int32).view(torch.float32)       # steps of 2^-149
+        w[:, :, at[near: near + zeros]] = 0.0
+        for budget in (1, zeros, zeros + 1, zeros + near - 1, zeros + near, zeros + near + 5):
+            check(cass, k.clone(), v.clone(), w.clone(), torch.tensor([cap], dtype=torch.int32, device="cuda"), budget, 0, 0)
+
+
 def test_a_budget_beyond_the_first_cache(cass):
     """Into a larger cache: everything stays."""
     k, v, w = make(3, 60, 2, 64)
