@@ -19,14 +19,14 @@ struct SaParts {
 
 // grid: (query heads, rows, sequences), WARPS warps a head: one where there are many pairs, more where there are few with many parts.
 // Bound: latency (two round trips behind the wait: where the parts lie, and the parts, eight of them together with a running maximum over
-// the rounds).  What runs once pays for each of its instructions, some 6 clocks: places by divisions in every block took 2 us more.
+// the rounds; four where a warp joins a head's, which has few parts then: 23680 pairs of 37 sequences 32 us by eight, 20 by four).  What runs once pays for each of its instructions, some 6 clocks: places by divisions in every block took 2 us more.
 constexpr int merge_threads(int warps) { return warps > 1 ? 32 * warps : 128; }
 
 template <int DT, int WARPS>
 __global__ void __launch_bounds__(merge_threads(WARPS)) k_shared_merge(SharedAttn a, int seg_shift, uint32_t group_magic, uint16_t* __restrict__ out,
                                                                        float* __restrict__ lse, int32_t* __restrict__ d_status) {
     using T = SaType<DT>;
-    constexpr int kWarps = merge_threads(WARPS) / 32, kParts = 8;
+    constexpr int kWarps = merge_threads(WARPS) / 32, kParts = WARPS == 1 ? 4 : 8;
     __shared__ __align__(16) float s_o[WARPS == 1 ? 1 : kWarps][256];
     __shared__ float2 s_ml[kWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -136,23 +136,30 @@ __global__ void __launch_bounds__(merge_threads(WARPS)) k_shared_merge(SharedAtt
     }
 }
 
-// The weights that the positions of the caches got: the scores' share of the sums.  grid: (blocks of 512 positions, KV heads, sequences).
-// The scores were there before the merge released this kernel; they travel while it finishes.
+// The weights that the positions of the caches got: the scores' share of the sums.  grid: (blocks of positions, KV heads, sequences).
+// The scores were there before the merge released this kernel; they travel while it finishes.  A thread takes four positions and all pairs, or
+// (SPLIT, more pairs than travel at a time) a warp takes every fourth pair: 80 pairs of 37 sequences of 146 positions 14.8 us without, 8.3 so;
+// 20 pairs of 16 sequences of 1000 7.5 and 6.0.
 constexpr int kSwThreads = 128, kSwPairs = 8, kSwMaxPairs = 256;
+constexpr int sw_positions(bool split) { return split ? 128 : kSwThreads * 4; }
 
+template <bool SPLIT>
 __global__ void __launch_bounds__(kSwThreads) k_shared_weights(SharedAttn a, const float* in, float* out) {
     __shared__ float s_lse[kSwMaxPairs];
     __shared__ int s_end[kSwMaxPairs];
+    __shared__ __align__(16) float s_sum[SPLIT ? kSwThreads / 32 : 1][SPLIT ? 128 : 4];
+    constexpr int kStep = SPLIT ? kSwThreads / 32 : 1;
     const int tid = threadIdx.x, head = blockIdx.y, b = blockIdx.z, P = a.rows * a.group;
-    const int n = shared_len(a, b), pos = (blockIdx.x * kSwThreads + tid) * 4;
+    const int first = SPLIT ? tid >> 5 : 0, base = blockIdx.x * sw_positions(SPLIT), pos = base + (SPLIT ? tid & 31 : tid) * 4;
+    const int n = shared_len(a, b);
     const int64_t row = (int64_t)b * a.n_kv + head;
     const float* from = a.scores + row * P * a.score_stride + min(pos, max(n - 1, 0) & ~3);
     float4 x[kSwPairs];
     auto load = [&](int q0) {
 #pragma unroll
-        for (int i = 0; i < kSwPairs; ++i) x[i] = *reinterpret_cast<const float4*>(from + (int64_t)min(q0 + i, P - 1) * a.score_stride);
+        for (int i = 0; i < kSwPairs; ++i) x[i] = *reinterpret_cast<const float4*>(from + (int64_t)min(q0 + i * kStep, P - 1) * a.score_stride);
     };
-    if (n > 0) load(0);
+    if (n > 0) load(first);
     pdl_wait();
     if (n < 0) return;                                   // the sequence is not there
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -162,13 +169,13 @@ __global__ void __launch_bounds__(kSwThreads) k_shared_weights(SharedAttn a, con
             s_end[q] = n - (a.rows - 1 - q / a.group);   // what the pair sees
         }
         __syncthreads();
-        for (int q0 = 0; q0 < P; q0 += kSwPairs) {
-            if (q0) load(q0);
+        for (int q0 = first; q0 < P; q0 += kSwPairs * kStep) {
+            if (q0 != first) load(q0);
 #pragma unroll
             for (int i = 0; i < kSwPairs; ++i) {
-                if (q0 + i >= P) break;
-                const int left = s_end[q0 + i] - pos;
-                const float z = s_lse[q0 + i], v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                if (q0 + i * kStep >= P) break;
+                const int left = s_end[q0 + i * kStep] - pos;
+                const float z = s_lse[q0 + i * kStep], v[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
                 for (int e = 0; e < 4; ++e) sum[e] += e < left ? exp2_fast(v[e] - z) : 0.f;
             }
@@ -176,9 +183,19 @@ __global__ void __launch_bounds__(kSwThreads) k_shared_weights(SharedAttn a, con
     }
     in = in ? in + row * a.capacity : nullptr;
     out += row * a.capacity;
+    if constexpr (SPLIT) {
+        *reinterpret_cast<float4*>(&s_sum[first][pos - base]) = make_float4(sum[0], sum[1], sum[2], sum[3]);
+        __syncthreads();
+        const int at = base + tid;
+        float all = 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        if (pos + i < a.capacity && (pos + i < n || in != out)) out[pos + i] = (in ? in[pos + i] : 0.f) + sum[i];
+        for (int i = 0; i < kStep; ++i) all += s_sum[i][tid];
+        if (at < a.capacity && (at < n || in != out)) out[at] = (in ? in[at] : 0.f) + all;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (pos + i < a.capacity && (pos + i < n || in != out)) out[pos + i] = (in ? in[pos + i] : 0.f) + sum[i];
+    }
 }
 
 // ---- host ----
@@ -227,7 +244,9 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     const int P = a.rows * group, all = a.n_seq * P;     // pairs of a sequence, of all
     plan->tc = a.prefix && shared_tc_usable(a) && (all > kSaStreamPairs || (int64_t)(all > 16 ? all : 16) * a.prefix * a.n_kv > kSaStreamWork);
     const int most = a.prefix && !plan->tc ? (all > P ? all : P) : P;
-    plan->mt = a.d > 128 || most <= 16 ? 1 : most <= 32 ? 2 : 4;
+    // Pairs a CTA takes at a time: 64 where a cache has so many that hardly any place is empty, else 32 in two CTAs an SM.  us, 64 and 32: a cache of
+    // 4000 behind 36 pairs 30.6, 33.5; 20 caches of 117 behind 64 21.9, 23.3; 6 of 2405 behind 80 104, 92; a prefix of 8000 behind 64 pairs of 96 dims 36.7, 33.4.
+    plan->mt = a.d > 128 || most <= 16 ? 1 : P > 32 && 2 * ceil_div(P, 64) == ceil_div(P, 32) ? 4 : 2;
     const int seg = 16 * plan->mt;
     a.pairs = most < seg ? most : seg;
     a.p_groups = a.prefix && !plan->tc ? ceil_div(all, seg) : 0;
@@ -272,8 +291,12 @@ static int run_shared(const SaPlan& plan, uint16_t* out, float* lse, const float
     else if (pairs <= kSmFewPairs && plan.levels > 1) CASS_SHARED_MERGE(16);
     else CASS_SHARED_MERGE(8);
 #undef CASS_SHARED_MERGE
-    if (weight_out)
-        CASS_PDL_LAUNCH(k_shared_weights, dim3(ceil_div(a.capacity, kSwThreads * 4), a.n_kv, a.n_seq), dim3(kSwThreads), 0, s, a, weight_in, weight_out);
+    if (weight_out) {
+        const bool split = a.rows * a.group > kSwPairs;
+        const dim3 grid(ceil_div(a.capacity, sw_positions(split)), a.n_kv, a.n_seq);
+        if (split) CASS_PDL_LAUNCH(k_shared_weights<true>, grid, dim3(kSwThreads), 0, s, a, weight_in, weight_out);
+        else CASS_PDL_LAUNCH(k_shared_weights<false>, grid, dim3(kSwThreads), 0, s, a, weight_in, weight_out);
+    }
     return CASS_OK;
 }
 
