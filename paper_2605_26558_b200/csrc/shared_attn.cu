@@ -207,7 +207,9 @@ struct SaPlan {
     size_t at_o, at_ml, at_slots, at_scores, at_lse, at_pre_o, at_pre_ml, bytes;
 };
 
-constexpr int kSmManyPairs = 4 * kSms;                   // joined by a warp each
+// Pairs from which on a warp joins one alone.  us of a call, by one warp and by eight: 256 pairs 23.7, 21.9; 384 25.8, 24.2; 512 27.6, 28.1; 768 31.9,
+// 33.4; 1536 40.4, 49.7.
+constexpr int kSmManyPairs = 3 * kSms;
 constexpr int kSmFewPairs = kSms / 2;                    // joined by 16 warps where a list is long: one cache of 32000 positions 37.8 -> 36.5 us; 256 pairs 20.3 -> 22.9
 // A prefix is streamed behind up to 32 pairs a KV head while (pairs, 16 at least) x positions x KV heads is below this: a launch less.
 // us, streamed and on the tensor cores, 8 KV heads of 128: 4 pairs, 4000 positions 12.5, 14.1; 32000 positions 35.0, 30.6; 16 pairs 13.5, 15.2
