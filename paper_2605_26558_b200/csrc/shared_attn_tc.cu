@@ -389,14 +389,10 @@ int64_t shared_tc_plan(SharedAttn& a) {
 
 // The prefix's K or V as [position][head][dim], whatever the order in memory, in boxes of 128 positions x 64 dims; zeros behind the last position.
 static int prefix_map(CUtensorMap* m, const SharedAttn& a, const uint16_t* at) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return CASS_ERR_CUDA;
     const cuuint64_t gdim[3] = {(cuuint64_t)a.d, (cuuint64_t)a.n_kv, (cuuint64_t)a.prefix};
     const cuuint64_t gstride[2] = {(cuuint64_t)(a.n_kv > 1 ? a.p_head : a.d) * 2, (cuuint64_t)(a.prefix > 1 ? a.p_pos : a.d) * 2};
-    const cuuint32_t box[3] = {64, 1, kStTile}, estr[3] = {1, 1, 1};
-    const CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(at), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? CASS_OK : CASS_ERR_INVALID_ARG;
+    const cuuint32_t box[3] = {64, 1, kStTile};
+    return tc_map(m, 3, at, gdim, gstride, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 template <int DT, int D>

@@ -528,16 +528,11 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
 
 // K or V as [sequence][head][position][dim], whatever the order in memory, in boxes of 32 positions.
 inline int shared_cache_map(CUtensorMap* map, const uint16_t* at, int d, int positions, int heads, int seqs, int64_t pos, int64_t head, int64_t seq) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return CASS_ERR_CUDA;
     const int width = d % 64 == 0 ? 64 : 32;
     const cuuint64_t dims[4] = {(cuuint64_t)d, (cuuint64_t)positions, (cuuint64_t)heads, (cuuint64_t)seqs};
     const cuuint64_t strides[3] = {(cuuint64_t)(positions > 1 ? pos : d) * 2, (cuuint64_t)(heads > 1 ? head : d) * 2, (cuuint64_t)(seqs > 1 ? seq : d) * 2};
-    const cuuint32_t box[4] = {(cuuint32_t)width, kSaBoxPos, 1, 1}, step[4] = {1, 1, 1, 1};
-    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<uint16_t*>(at), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? CASS_OK : CASS_ERR_INVALID_ARG;
+    const cuuint32_t box[4] = {(cuuint32_t)width, kSaBoxPos, 1, 1};
+    return tc_map(map, 4, at, dims, strides, box, width == 64 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B);
 }
 
 template <int DT, int D, int MT>

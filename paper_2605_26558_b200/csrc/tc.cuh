@@ -22,31 +22,41 @@ inline EncodeTiledFn encode_fn() {
     return fn;
 }
 
+// Map over 16-bit values, zero fill outside; dims[0] is contiguous, strides (bytes) are those of dims[1..].  A host thread that has made no
+// call yet that needs the device's context has none bound, and the encoder refuses it: it is bound then, and the encoder asked again.
+inline int tc_map(CUtensorMap* m, int rank, const void* at, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+                  CUtensorMapSwizzle swizzle) {
+    const EncodeTiledFn fn = encode_fn();
+    if (!fn) return CASS_ERR_CUDA;
+    const cuuint32_t step[5] = {1, 1, 1, 1, 1};
+    auto encode = [&]() {
+        return fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(at), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r == CUDA_ERROR_INVALID_CONTEXT || r == CUDA_ERROR_NOT_INITIALIZED) {
+        int dev = 0;
+        CASS_CUDA_CHECK(cudaGetDevice(&dev));
+        CASS_CUDA_CHECK(cudaSetDevice(dev));
+        r = encode();
+    }
+    return r == CUDA_SUCCESS ? CASS_OK : CASS_ERR_INVALID_ARG;
+}
+
 // bf16 matrix [rows][cols] row-major -> map with a (box_rows x 64)-element box, 128-byte swizzle, zero fill outside.
 inline int tc_matrix_map(CUtensorMap* m, const void* ptr, int rows, int cols, int box_rows) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return CASS_ERR_CUDA;
-    cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows};
-    cuuint64_t gstride[1] = {(cuuint64_t)cols * 2};
-    cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
-    cuuint32_t estr[2] = {1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(ptr), gdim, gstride, box, estr,
-                    CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                    CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? CASS_OK : CASS_ERR_INVALID_ARG;
+    const cuuint64_t gdim[2] = {(cuuint64_t)cols, (cuuint64_t)rows}, gstride[1] = {(cuuint64_t)cols * 2};
+    const cuuint32_t box[2] = {64, (cuuint32_t)box_rows};
+    return tc_map(m, 2, ptr, gdim, gstride, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 // Sequence 0's bf16 K or V cache of one layer ([max_seq][n_kv][128]; the other sequences lie seq_stride bytes apart) -> map over
 // [dim, position, sequence] with a box of 64 dims x 128 positions.
 inline int tc_cache_map(CUtensorMap* m, const KvGeom& g, const uint16_t* cache, int n_seq) {
-    EncodeTiledFn fn = encode_fn();
-    if (!fn) return CASS_ERR_CUDA;
     const cuuint64_t gdim[3] = {(cuuint64_t)g.n_kv * g.d, (cuuint64_t)g.max_seq, (cuuint64_t)n_seq};
     const cuuint64_t gstride[2] = {(cuuint64_t)g.n_kv * g.d * 2, (cuuint64_t)(n_seq > 1 ? g.seq_stride : (size_t)g.max_seq * g.n_kv * g.d * 2)};
-    const cuuint32_t box[3] = {64, 128, 1}, estr[3] = {1, 1, 1};
-    CUresult r = fn(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<uint16_t*>(cache), gdim, gstride, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    return r == CUDA_SUCCESS ? CASS_OK : CASS_ERR_INVALID_ARG;
+    const cuuint32_t box[3] = {64, 128, 1};
+    return tc_map(m, 3, cache, gdim, gstride, box, CU_TENSOR_MAP_SWIZZLE_128B);
 }
 
 __device__ __forceinline__ void tma_load_2d(void* smem_dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
