@@ -8,6 +8,11 @@
 namespace cass {
 
 // ---- 16-bit types ----
+// Numerators of the softmax are rounded to the type for the second product, half a step of each (2^-8 of it in bf16, 2^-11 in fp16): an output
+// is off by less than such a step of the values' weighted sizes, as its own rounding is, and the products run at the 16-bit rate.  Their sums stay
+// in 32 bits and are of the numerators before that.  fp16 has no exponents for a long flat tail behind a favoured position (below 2^-14 of the
+// maximum its steps stay the same, below 2^-25 there is nothing), so its numerators are relative to 2^-lift of the base and reach 2^15, with
+// the kernels' room for growth; parts carry the base so lowered as their maximum, and the merge needs not know.
 template <int DT> struct SaType;
 template <> struct SaType<CASS_BF16> {
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -20,6 +25,8 @@ template <> struct SaType<CASS_BF16> {
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     }
     static constexpr uint32_t kExponent = 0x7F80u;
+    static constexpr float kGrowth = 8.f;                // powers of two that numerators may grow over their base before what was summed is rescaled
+    static constexpr float kLift = 0.f;                  // of numerators that are rescaled at every new maximum
     static __device__ __forceinline__ float get(uint32_t v) { return __uint_as_float(v << 16); }
     static __device__ __forceinline__ uint16_t put(float v) { return float_to_bf16_bits(v); }
 };
@@ -34,6 +41,8 @@ template <> struct SaType<CASS_F16> {
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
     }
     static constexpr uint32_t kExponent = 0x7C00u;
+    static constexpr float kGrowth = 4.f;                // (with 8, and no lift: 64 sequences of 40 heads behind 32768 positions 90.3 us, so 92.8)
+    static constexpr float kLift = 15.f;
     static __device__ __forceinline__ float get(uint32_t v) { return __half2float(__ushort_as_half((uint16_t)v)); }
     static __device__ __forceinline__ uint16_t put(float v) { return __half_as_ushort(__float2half_rn(v)); }
 };

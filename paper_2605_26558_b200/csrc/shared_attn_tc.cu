@@ -3,8 +3,8 @@
 // A CTA holds the queries of one or two tiles of a KV head and takes a range of the prefix through both products:
 //   scores [128 pairs x 128 positions] = Q K^T, in tensor memory; softmax numerators P over them, 16 bits; output [128 pairs x d] += P V.
 // A pair is a lane of tensor memory and a thread, so the softmax crosses no threads.  The output stays in tensor memory; it is rescaled only
-// when a pair's maximum has grown by more than 2^8 since the base that its numerators are relative to (they then reach 256, which both
-// 16-bit types hold as exactly as 1), which after the first tiles hardly happens.  Two warpgroups alternate on the tensor cores: with two tiles of
+// when a pair's maximum has grown by more than 2^8 (fp16: 2^4) since the base that its numerators are relative to, which after the first
+// tiles hardly happens.  Two warpgroups alternate on the tensor cores: with two tiles of
 // pairs each has one, and both use the same K and V; with one they take the positions' tiles in turn.  While one's numerators are formed
 // the other's products run.
 // Bound: with one tile of pairs K and V bytes, 1.31 us for the 64 KB of 128 positions on every SM, 7.4 TB/s.  With two, the chain of
@@ -21,7 +21,6 @@ constexpr int kStRegsLaunch = 168, kStRegsIssue = 56, kStRegsSoftmax = 224;     
 static_assert(128 * kStRegsIssue + 256 * kStRegsSoftmax <= kStThreads * kStRegsLaunch, "the shares come from what the block was launched with");
 constexpr uint32_t kStS = 0, kStO = 256;                 // tensor memory: two score (and P) buffers, two outputs, 128 columns each
 constexpr int kStFewTiles = 4;                           // (tiles of pairs, of positions) an SM up to which SMs are left to the streaming kernel
-constexpr float kStGrowth = 8.f;                         // of a maximum, in powers of two, before what came before is rescaled
 
 template <int D>
 struct StShape {
@@ -87,6 +86,8 @@ template <int DT, int D>
 __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                                     SharedAttn a, int32_t* __restrict__ d_status) {
     using S = StShape<D>;
+    using T = SaType<DT>;
+    constexpr float kLift = T::kLift > 0.f ? T::kLift - T::kGrowth : 0.f;        // numerators may outgrow the base
     constexpr int kBoxes = D / 64, kTile = S::q_tile, kBox = kStTile * 64 * 2;
     extern __shared__ uint8_t smem_dyn[];
     uint8_t* base = reinterpret_cast<uint8_t*>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
@@ -277,7 +278,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
 #pragma unroll
             for (int c = 4; c < 128; ++c) x[c & 3] = fmaxf(x[c & 3], s[c]);
             const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * a.scale_log2;      // (the scale is positive)
-            const bool grew = top > m + kStGrowth;       // also from -inf
+            const bool grew = top > m + T::kGrowth;       // also from -inf
             if (__any_sync(0xffffffffu, grew)) {
                 const float fix = grew ? st_exp2(m - top) : 1.f;
                 if (grew) m = top;
@@ -295,7 +296,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
                     }
                 }
             }
-            const float from = m == -INFINITY ? 0.f : m;
+            const float from = (m == -INFINITY ? 0.f : m) - kLift;
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < 128; c += 64) {
@@ -321,7 +322,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
             const int all = first + (two ? wg * kStTile : 0) + row;
             const int64_t at = two ? (((int64_t)split * a.n_kv + head) * a.pre_n2 + cta) * 2 * kStTile + wg * kStTile + row
                                    : a.pre_at1 + ((int64_t)(2 * split + wg) * a.n_kv + head) * kStTile + row;
-            if (all < P) a.pre_ml[at] = make_float2(m, l);
+            if (all < P) a.pre_ml[at] = make_float2(m - kLift, l);
             // through the ring (every product that read it is done), so that a warp's stores are whole rows
             float4* box = reinterpret_cast<float4*>(sT) + (warp - 4) * 32 * (D / 4);
 #pragma unroll

@@ -381,6 +381,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                 x = fmaxf(m[k], x * a.scale_log2);           // (the scale is positive)
                 base[k] = x == -INFINITY ? 0.f : x;
                 fix[k] = exp2_fast(m[k] - base[k]);
+                base[k] -= T::kLift;
                 grew |= x != m[k];
                 m[k] = x;
             }
@@ -518,7 +519,7 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                 }
                 if (p < P) *reinterpret_cast<float2*>(part + (int64_t)8 * h * D + k * 8) = x;
             }
-            if (set == 0 && p < P && (lane & 3) == 0) a.part_ml[(int64_t)run.slot * a.pairs + p] = make_float2(all[h], sum[h]);
+            if (set == 0 && p < P && (lane & 3) == 0) a.part_ml[(int64_t)run.slot * a.pairs + p] = make_float2(all[h] - T::kLift, sum[h]);
         }
         fence_proxy_async();
         arrive(release);
