@@ -260,9 +260,10 @@ static int run_rope(RopeArgs a, const double* freqs, const int32_t* positions, c
         if (a.per_cta > fit) a.per_cta = fit > 1 ? fit : 1;
     }
     // few rows: all SMs before full CTAs (148 rows of 40 heads of 128: 4.7 us by full CTAs, 3.1 so)
-    if (a.per_cta > ceil_div(a.rows, kSms)) a.per_cta = ceil_div(a.rows, kSms);
+    const auto groups = [&](int of) { return (int)(((int64_t)a.rows + of - 1) / of); };          // (rows may be 2^31 - 1)
+    if (a.per_cta > groups(kSms)) a.per_cta = groups(kSms);
     const size_t smem = (size_t)a.per_cta * half * sizeof(float2);
-    const dim3 grid(ceil_div(a.rows, a.per_cta));
+    const dim3 grid(groups(a.per_cta));
     if (a.g.interleaved)
         CASS_PDL_LAUNCH((k_rope<T, V, true>), grid, dim3(kRopeThreads), smem, s, a, freqs, positions, (const T*)q, (const T*)k, (T*)q_out, (T*)k_out);
     else

@@ -1,0 +1,32 @@
+"""Rotary positions at the ends of what a call may be: the most rows, none."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def cass():
+    import paper_2605_26558_b200 as m
+    return m
+
+
+def test_as_many_rows_as_a_call_takes(cass):
+    """2^31 - 1 rows of one head, in place, the row its position.  Tolerances: a turn as in test_gpu_rope.py (6 x 2^-24 of |a| + |b|, a few 2^-53 of the
+    angle), the result rounded to the type (half a step, 2^-25 at least)."""
+    rows = 2 ** 31 - 1
+    if torch.cuda.mem_get_info()[0] < 12 << 30:
+        pytest.skip("no room for that many rows")
+    x = torch.zeros(rows, 1, 2, dtype=torch.float16, device="cuda")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    at = torch.cat([torch.arange(1000), torch.randint(0, rows, (1000,)), torch.arange(rows - 1000, rows)]).unique().cuda()
+    x[at] = torch.randn(len(at), 1, 2, generator=g, device="cuda").half()
+    before = x[at].double()
+    freqs = torch.tensor([0.7, 1.0], dtype=torch.float64, device="cuda")
+    geom = cass.RopeGeom(cass.F16, 2, 2, 0, 1, 0, 2, 2, 0, 0, 2, 2, 0, 0)
+    cass.cass_rope(geom, freqs, None, rows, x, None, x, None)
+    t = at.double() * 0.7
+    a, b = before[:, 0, 0], before[:, 0, 1]
+    want = torch.stack((a * t.cos() - b * t.sin(), a * t.sin() + b * t.cos()), 1)
+    tol = (a.abs() + b.abs())[:, None] * (6 * 2.0 ** -24 + t[:, None] * 4 * 2.0 ** -53) + want.abs() * 2.0 ** -11 * (1 + 2.0 ** -10) + 2.0 ** -25
+    assert ((x[at][:, 0].double() - want).abs() <= tol).all()
