@@ -312,8 +312,11 @@ extern "C" int cass_rope(const cass_rope_geom* geom, const double* freqs, const 
     if (g.dtype != CASS_BF16 && g.dtype != CASS_F16 && g.dtype != CASS_F32) return CASS_ERR_INVALID_ARG;
     if (g.rot_dim < 2 || g.rot_dim % 2 || g.head_dim < g.rot_dim || g.n_q_heads < 0 || g.n_k_heads < 0) return CASS_ERR_INVALID_ARG;
     if (g.rot_dim > 4096) return CASS_ERR_UNSUPPORTED;                   // one row's sines and cosines in shared memory
-    if ((g.n_q_heads > 0) != (q != nullptr) || (g.n_k_heads > 0) != (k != nullptr) || (!q && !k)) return CASS_ERR_INVALID_ARG;
-    if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return CASS_ERR_INVALID_ARG;
+    if (g.n_q_heads == 0 && g.n_k_heads == 0) return CASS_ERR_INVALID_ARG;
+    if (rows > 0) {                                                      // (tensors without rows have no address)
+        if ((g.n_q_heads > 0) != (q != nullptr) || (g.n_k_heads > 0) != (k != nullptr)) return CASS_ERR_INVALID_ARG;
+        if ((q != nullptr) != (q_out != nullptr) || (k != nullptr) != (k_out != nullptr)) return CASS_ERR_INVALID_ARG;
+    }
     const int64_t heads = (int64_t)g.n_q_heads + g.n_k_heads;
     if (heads > 65535 || heads * rows > 0x7FFFFFFFll) return CASS_ERR_UNSUPPORTED;
     const uintptr_t size = g.dtype == CASS_F32 ? 4 : 2;
