@@ -447,7 +447,8 @@ int cass_shared_prefix_attention(const cass_cache_geom* cache, const cass_shared
  * [capacity of the output], the weights of what stays, then zeros up to the capacity.  Rows of K and V behind what stays are left as
  * they were.  A sequence whose length is outside 0 .. capacity is left alone: its `kept` is -1, its new_lens its length, its
  * caches and weights are not written.
- * 1 <= budget <= capacity (of the output); n_first, n_last >= 0, n_first + n_last <= budget.  head_dim a multiple of 8, at most 512. */
+ * 1 <= budget <= capacity (of the output); n_first, n_last >= 0, n_first + n_last <= budget.  head_dim a multiple of 8, at most 512;
+ * n_seq and n_kv_heads up to 65535; budget, and the output's capacity if weight_out is given, up to 2^31 - 2^16; CASS_ERR_UNSUPPORTED otherwise. */
 int cass_kv_evict(const cass_cache_geom* cache, void* k_cache, void* v_cache, const float* weight, const int32_t* lens, int budget,
                   int n_first, int n_last, const cass_cache_geom* cache_out, void* k_out, void* v_out, float* weight_out, int32_t* kept,
                   int32_t* new_lens, void* stream);

@@ -18,6 +18,7 @@ namespace cass {
 constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvMaxCluster = 8;
+constexpr int kEvMaxOut = 0x7FFFFFFF - 0xFFFF;           // positions that stay, or of a cache whose weights are written: loops step past them in 32 bits
 constexpr uint32_t kEvZero = 0x80000000u;                // key of a weight of 0
 
 struct EvictArgs {
@@ -61,7 +62,7 @@ __global__ void __launch_bounds__(kEvThreads) k_evict_select(EvictArgs a, const 
         return;
     }
     const int mid = n - a.n_first - a.n_last, take = a.budget - a.n_first - a.n_last;      // take < mid
-    const int per = ceil_div(mid, cs), lo = min(rank * per, mid), m = min(per, mid - lo);  // this CTA's part of the middle
+    const int per = (mid - 1) / cs + 1, lo = min(rank * per, mid), m = min(per, mid - lo);  // this CTA's part of the middle
     const int piece = KEYS ? KEYS * 32 : ceil_div(ceil_div(m, kEvWarps), 32) * 32, w0 = min(warp * piece, m), w1 = min(w0 + piece, m);
     const float* w = weight + at * a.capacity + a.n_first + lo;
     uint32_t keys[KEYS ? KEYS : 1];
@@ -296,8 +297,9 @@ bool cache_geom_ok(const cass_cache_geom& g, bool any) {
 // keys would not fit the registers (32 heads of 32768 by four CTAs of 8 keys a thread 37.0 us, by one of 32 74).
 static int evict_cluster(const EvictArgs& a, int n_seq) {
     int cs = 1;
-    while (cs < kEvMaxCluster && a.capacity / (cs * 2) >= 4 * kEvThreads && (int64_t)n_seq * a.n_kv * cs * 2 <= kSms) cs *= 2;
-    while (cs < kEvMaxCluster && ceil_div(a.capacity, cs) > kEvThreads * 16) cs *= 2;
+    const int64_t capacity = a.capacity;                 // up to 2^31 - 1
+    while (cs < kEvMaxCluster && capacity / (cs * 2) >= 4 * kEvThreads && (int64_t)n_seq * a.n_kv * cs * 2 <= kSms) cs *= 2;
+    while (cs < kEvMaxCluster && capacity > (int64_t)cs * kEvThreads * 16) cs *= 2;
     return cs;
 }
 
@@ -334,9 +336,10 @@ extern "C" int cass_kv_evict(const cass_cache_geom* cache, void* k_cache, void* 
     if (((uintptr_t)weight | (uintptr_t)weight_out | (uintptr_t)lens | (uintptr_t)kept | (uintptr_t)new_lens) & 3) return CASS_ERR_INVALID_ARG;
     if (weight_out == weight && o.capacity != g.capacity && g.n_seq * (int64_t)g.n_kv_heads > 1) return CASS_ERR_INVALID_ARG;
     if (g.head_dim % 8 || g.head_dim > 512 || g.n_seq > 65535 || g.n_kv_heads > 65535) return CASS_ERR_UNSUPPORTED;
+    if (budget > kEvMaxOut || (weight_out && o.capacity > kEvMaxOut)) return CASS_ERR_UNSUPPORTED;
     cudaStream_t s = (cudaStream_t)stream_;
     const EvictArgs a{g.n_kv_heads, g.capacity, budget, n_first, n_last};
-    const int cs = evict_cluster(a, g.n_seq), per = ceil_div(g.capacity, cs);
+    const int cs = evict_cluster(a, g.n_seq), per = (g.capacity - 1) / cs + 1;
     const int rc = per <= kEvThreads       ? launch_select<1>(a, g.n_seq, cs, weight, lens, kept, s)
                    : per <= 2 * kEvThreads  ? launch_select<2>(a, g.n_seq, cs, weight, lens, kept, s)
                    : per <= 4 * kEvThreads  ? launch_select<4>(a, g.n_seq, cs, weight, lens, kept, s)

@@ -23,3 +23,14 @@ def test_a_rotation_of_no_rows_does_nothing(cass, nq, nk):
     assert cass.lib.cass_rope(C.byref(g), C.c_void_p(AT), None, 1, None, None, None, None, 0, None) == cass.ERR_INVALID_ARG
     g.n_q_heads = g.n_k_heads = 0
     assert cass.lib.cass_rope(C.byref(g), C.c_void_p(AT), None, 0, None, None, None, None, 0, None) == cass.ERR_INVALID_ARG
+
+
+def test_evictions_that_keep_more_than_32_bits_of_steps(cass):
+    most = 2 ** 31 - 2 ** 16
+    p = lambda i: C.c_void_p(AT + (i << 24))  # noqa: E731
+
+    def call(capacity, budget, weight_out=None):
+        c = cass.CacheGeom(cass.BF16, 1, 1, 8, capacity, 0, 8, 0)
+        return cass.lib.cass_kv_evict(C.byref(c), p(0), p(1), p(2), p(3), budget, 0, 0, None, None, None, weight_out, p(4), p(5), None)
+
+    assert call(2 ** 31 - 1, most + 1) == call(most + 1, 100, p(6)) == cass.ERR_UNSUPPORTED
