@@ -82,7 +82,10 @@ class Engine:
         self.n_prompt = 0
 
     def set_rope(self, params: B.RopeParams):
-        """Rotary positions scaled for longer contexts (see cass_rope_params); before the first prefill, or after reset()."""
+        """Rotary positions scaled for longer contexts (see cass_rope_params); before the first prefill, or after reset(): keys that
+        are in the caches were turned by the old ones (CASS_ERR_INVALID_ARG)."""
+        if any(self.lens()):
+            raise B.CassError("Engine.set_rope (the caches hold positions)", B.ERR_INVALID_ARG)
         B.cass_session_set_rope(self.session, params)
 
     def prefill(self, prompt: torch.Tensor, calibrate: bool = False):

@@ -1,4 +1,4 @@
-"""Rotary positions at the ends of what a call may be: the most rows, none."""
+"""Rotary positions at the ends of what a call may be: the most rows; a session's tables by the definition, and when they may change."""
 import pytest
 import torch
 
@@ -30,3 +30,23 @@ def test_as_many_rows_as_a_call_takes(cass):
     want = torch.stack((a * t.cos() - b * t.sin(), a * t.sin() + b * t.cos()), 1)
     tol = (a.abs() + b.abs())[:, None] * (6 * 2.0 ** -24 + t[:, None] * 4 * 2.0 ** -53) + want.abs() * 2.0 ** -11 * (1 + 2.0 ** -10) + 2.0 ** -25
     assert ((x[at][:, 0].double() - want).abs() <= tol).all()
+
+
+def test_engine_turns_by_other_frequencies_only_while_its_caches_are_empty(cass):
+    import dataclasses
+
+    import synth
+    from paper_2605_26558_b200 import engine
+    shape = dataclasses.replace(synth.TINY, n_layers=1)
+    w = synth.model_weights(shape, 5, "cuda")
+    w["layers"] = [engine.fuse_layer_weights(lw) for lw in w["layers"]]
+    eng = engine.Engine(shape, w, max_seq=128)
+    params = cass.RopeParams(shape.head_dim, cass.ROPE_LINEAR, shape.rope_theta, 2.0, 1.0, 4.0, 64.0, 0.0)
+    eng.set_rope(params)
+    eng.prefill(synth.random_prompt(20, shape.vocab, 4))
+    with pytest.raises(cass.CassError) as e:
+        eng.set_rope(params)
+    assert e.value.code == cass.ERR_INVALID_ARG
+    eng.reset()
+    eng.set_rope(params)
+    eng.close()

@@ -34,3 +34,20 @@ def test_evictions_that_keep_more_than_32_bits_of_steps(cass):
         return cass.lib.cass_kv_evict(C.byref(c), p(0), p(1), p(2), p(3), budget, 0, 0, None, None, None, weight_out, p(4), p(5), None)
 
     assert call(2 ** 31 - 1, most + 1) == call(most + 1, 100, p(6)) == cass.ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("lens", [[0], [7], [0, 0], [0, 3]])
+def test_an_engine_with_positions_in_its_caches_keeps_its_rotation(cass, monkeypatch, lens):
+    from paper_2605_26558_b200 import engine
+    calls = []
+    monkeypatch.setattr(engine.B, "cass_session_lens", lambda session, batch: lens)
+    monkeypatch.setattr(engine.B, "cass_session_set_rope", lambda session, params: calls.append(params))
+    eng = object.__new__(engine.Engine)
+    eng.session, eng.batch, eng.n_prompt = None, len(lens), 0
+    if any(lens):
+        with pytest.raises(cass.CassError) as e:
+            eng.set_rope("params")
+        assert e.value.code == cass.ERR_INVALID_ARG and not calls
+    else:
+        eng.set_rope("params")
+        assert calls == ["params"]
