@@ -50,3 +50,36 @@ def test_engine_turns_by_other_frequencies_only_while_its_caches_are_empty(cass)
     eng.reset()
     eng.set_rope(params)
     eng.close()
+
+
+@pytest.mark.parametrize("kind", ["none", "linear", "ntk", "bands", "yarn"])
+@pytest.mark.parametrize("factor", [2.0, 8.0])
+def test_a_session_turns_by_the_definition(cass, kind, factor):
+    """q and k of a verification of one token at positions 0 to 8: unscaled, its first row is the unturned one (rounded to 16 bits before the
+    rotation), and every row of a scaled session is that one turned by the definition's angle.  Tolerances of test_gpu_rope.py."""
+    import dataclasses
+
+    import synth
+    import test_gpu_rope
+    from paper_2605_26558_b200 import engine
+    shape = dataclasses.replace(synth.TINY, n_layers=1)
+    w = synth.model_weights(shape, 5, "cuda")
+    w["layers"] = [engine.fuse_layer_weights(lw) for lw in w["layers"]]
+    eng = engine.Engine(shape, w, max_seq=128)
+    rows, d, heads = 9, shape.head_dim, shape.n_q_heads + shape.n_kv_heads
+    toks = torch.full((1, rows), 77, device="cuda", dtype=torch.int32)
+
+    def turned():
+        eng.reset()
+        cass.cass_verify(eng.session, toks, rows - 1, torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, shape.vocab, device="cuda"))
+        ptr, _, cols = cass.cass_debug_activation(eng.session, 2)
+        o = ptr - eng.mem.data_ptr()
+        return eng.mem[o: o + 2 * rows * cols].view(torch.bfloat16).view(rows, -1, d)[:, :heads].clone()
+
+    x = turned()[:1].expand(rows, -1, -1)
+    eng.reset()
+    which = ("none", "linear", "ntk", "bands", "yarn").index(kind)
+    eng.set_rope(cass.RopeParams(d, which, shape.rope_theta, factor, 1.0, 4.0, 64.0, 0.0))
+    freqs, gain = test_gpu_rope.frequencies(d, kind, shape.rope_theta, factor, 1.0, 4.0, 64.0)
+    test_gpu_rope.check(turned(), x, torch.arange(rows, device="cuda"), freqs, gain, False, 0)
+    eng.close()
