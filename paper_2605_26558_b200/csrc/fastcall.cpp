@@ -66,6 +66,43 @@ bool elsewhere(PyObject* o) {
     return true;
 }
 
+bool mistyped(PyObject* o, at::ScalarType want, bool bits_too) {
+    if (!THPVariable_Check(o)) return false;
+    const at::ScalarType is = THPVariable_Unpack(o).scalar_type();
+    if (is == want || (bits_too && !at::isFloatingType(is))) return false;
+    PyErr_Format(PyExc_TypeError, "tensor of %s where %s is wanted", c10::toString(is), c10::toString(want));
+    return true;
+}
+
+// The type that a description names for the values it describes; Undefined: none.
+template <class T>
+at::ScalarType described(PyObject* o) {
+    using P = std::remove_cv_t<std::remove_pointer_t<T>>;
+    void* at = nullptr;
+    if constexpr (std::is_same_v<P, cass_cache_geom> || std::is_same_v<P, cass_rope_geom>) {
+        if (buffer_address(o, sizeof(P), &at)) {
+            const int type = static_cast<const P*>(at)->dtype;
+            return type == CASS_BF16 ? at::kBFloat16 : type == CASS_F16 ? at::kHalf : type == CASS_F32 ? at::kFloat : at::ScalarType::Undefined;
+        }
+        PyErr_Clear();                     // said when the argument is converted
+    }
+    return at::ScalarType::Undefined;
+}
+
+// A tensor of another type than parameter T's elements, or than the description's values where T is untyped; NEXT: the parameter behind it (a
+// size: T is scratch, of any type).  Raw bits in whole numbers pass for values.
+template <class T, class NEXT>
+bool wrong_type(PyObject* o, at::ScalarType values) {
+    if constexpr (std::is_pointer_v<T>) {
+        using P = std::remove_cv_t<std::remove_pointer_t<T>>;
+        if constexpr (std::is_same_v<P, int32_t>) return mistyped(o, at::kInt, false);
+        else if constexpr (std::is_same_v<P, float>) return mistyped(o, at::kFloat, false);
+        else if constexpr (std::is_same_v<P, double>) return mistyped(o, at::kDouble, false);
+        else if constexpr (std::is_void_v<P> && !std::is_same_v<NEXT, size_t>) return values != at::ScalarType::Undefined && mistyped(o, values, true);
+    }
+    return false;
+}
+
 bool stream_handle(PyObject* o, void** out) {
     static bool initialised = false;       // under the interpreter lock
     if (o == Py_None && initialised) {
@@ -109,7 +146,7 @@ bool argument(PyObject* o, T* out) {
     else return convert(o, out);
 }
 
-// HERE: tensors have to be on the current device.
+// HERE: tensors have to be on the current device, and of the parameters' types.
 template <auto F, bool HERE = false>
 struct Entry;
 template <class... A, int (*F)(A...), bool HERE>
@@ -118,7 +155,12 @@ struct Entry<F, HERE> {
     template <size_t... I>
     static PyObject* run(PyObject* const* args, std::index_sequence<I...>) {
         std::tuple<A...> v;
-        if (HERE && (elsewhere(args[I]) || ...)) return nullptr;
+        if constexpr (HERE) {
+            using Next = std::tuple<A..., void>;
+            const at::ScalarType values = described<std::tuple_element_t<0, std::tuple<A...>>>(args[0]);
+            if ((wrong_type<A, std::tuple_element_t<I + 1, Next>>(args[I], values) || ...)) return nullptr;
+            if ((elsewhere(args[I]) || ...)) return nullptr;
+        }
         if (!(argument<I + 1 == N>(args[I], &std::get<I>(v)) && ...)) return nullptr;
         int rc;
         Py_BEGIN_ALLOW_THREADS

@@ -51,3 +51,31 @@ def test_an_engine_with_positions_in_its_caches_keeps_its_rotation(cass, monkeyp
     else:
         eng.set_rope("params")
         assert calls == ["params"]
+
+
+def test_tensors_of_other_types_are_refused(cass):
+    """A length in torch's own 64-bit integers would be read as two 32-bit ones, 32-bit values as pairs of 16-bit ones.  (Tensors of the host:
+    with the right types it is their place that is refused.)"""
+    import torch
+    i32, f32, f64 = (torch.zeros(8, dtype=t) for t in (torch.int32, torch.float32, torch.float64))
+    half, bf = torch.zeros(64, dtype=torch.float16), torch.zeros(64, dtype=torch.bfloat16)
+    i64, bits = torch.zeros(8, dtype=torch.int64), torch.zeros(64, dtype=torch.int16)
+    cache = cass.CacheGeom(cass.BF16, 1, 1, 32, 2, 64, 32, 32)
+    attn = cass.SharedAttn(1, 1, 32, 32, 32, 32, 32, 32, 2, 32, 32, 0.0)
+    geom = cass.RopeGeom(cass.F32, 4, 4, 0, 1, 0, 4, 4, 0, 0, 4, 4, 0, 0)
+
+    def refused(call, good, bad):
+        """Every argument of `bad` in turn instead of the one of `good`."""
+        with pytest.raises(AssertionError):
+            call(*good)
+        for at, wrong in bad.items():
+            for x in wrong:
+                with pytest.raises(TypeError, match="tensor of"):
+                    call(*good[:at], x, *good[at + 1:])
+
+    refused(cass.cass_rope, [geom, f64, i32, 2, f32, None, f32, None], {1: [f32], 2: [i64, f32], 4: [half, f64], 6: [bf]})
+    refused(cass.cass_rope_freqs, [cass.RopeParams(4, 0, 1e4, 1.0, 1.0, 4.0, 64.0, 0.0), f64], {1: [f32]})
+    refused(cass.cass_shared_prefix_attention, [cache, attn, bf, bf, bf, bf, bits, i32, bf, f32, f32, f32, f32, 32, i32],
+            {2: [half, f32], 3: [half], 6: [half], 7: [i64], 8: [f32], 9: [f64, half], 10: [f64], 11: [bf], 14: [i64]})
+    refused(cass.cass_kv_evict, [cache, bf, bits, f32, i32, 1, 0, 0, cache, bf, bf, f32, i32, i32],
+            {1: [half], 2: [f32], 3: [f64], 4: [i64], 9: [half], 11: [bf], 12: [i64], 13: [i64]})
