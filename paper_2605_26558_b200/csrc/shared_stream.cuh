@@ -241,7 +241,8 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
             asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(smem_u32(&r_full[slot])) : "memory");
         };
         // CTAs of the grid are pieces: the first of every span, then the second of every span, ...
-        for (int cta = blockIdx.x, ctas = 0; cta >= 0 && ok; ++ctas) {
+        int cta = blockIdx.x, ctas = 0;
+        for (; cta >= 0 && ok; ++ctas) {
             const int level = cta / a.ctas, w = cta - level * a.ctas, piece = w * list.levels + level;
             const int first = shared_span(list, w), tiles = shared_span(list, w + 1) - first;
             const int t0 = first + shared_cut(list, tiles, level), t1 = level < list.levels ? first + shared_cut(list, tiles, level + 1) : t0;
@@ -269,8 +270,10 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
             __syncwarp();
         }
         if (ok) tell(0, 0, -1);
-        if (!ok)                                         // what is in flight lands before the CTA ends (bounded)
+        if (!ok) {                                       // what is in flight lands before the CTA ends (bounded): copies, and the last question's answer
             for (int i = max(left - S::stages, 0); i < left; ++i) mbar_wait_bounded(&full[i % S::stages], (uint32_t)(i / S::stages) & 1u);
+            mbar_wait_bounded(&answered, (uint32_t)(ctas - 1) & 1u);
+        }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (a.behind_tc) pdl_wait();
         return;

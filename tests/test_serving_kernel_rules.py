@@ -1,0 +1,19 @@
+"""What the serving kernels do when a bounded wait runs out, and with what they read then: read from the sources or run on the host, as
+making one run out would leave a GPU with work of a block that has ended."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2605_26558_b200", "csrc")
+
+
+def _code(name):
+    return re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, name)).read())
+
+
+def test_a_block_that_gives_up_waits_for_the_answer_it_asked_for():
+    """The hardware's answer to clusterlaunchcontrol is 16 bytes written to the block's shared memory: every way out waits for it."""
+    code = _code("shared_stream.cuh")
+    loop = code.index("for (; cta >= 0 && ok;") if "for (; cta >= 0 && ok;" in code else code.index("for (int cta = blockIdx.x")
+    after = code[loop:code.index("if (a.behind_tc) pdl_wait();", loop)]
+    failed = after[after.rindex("if (!ok)"):]
+    assert re.search(r"mbar_wait_bounded\(&answered, ", failed), failed
