@@ -418,12 +418,11 @@ __global__ void __launch_bounds__(SaShape<D, MT>::threads, SaShape<D, MT>::per_s
                 }
                 // (The warps of these positions find the same.  They meet at a barrier with a bounded wait: after a wait that ran out they
                 // may have read different things.)
-                auto sync_set = [&](uint32_t parity) {       // two of them each time: phases 0 and 1
+                auto sync_set = [&](uint32_t phase) {        // two of them each time: phases 0 and 1
                     __syncwarp();
                     if (MT > 1) {
                         if (lane == 0) asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_u32(&meet[set])) : "memory");
-                        mbar_wait_bounded(&meet[set], parity);
-                        __syncwarp();
+                        wait(&meet[set], phase);
                     }
                 };
                 if (__any_sync(0xffffffffu, odd)) {

@@ -17,3 +17,11 @@ def test_a_block_that_gives_up_waits_for_the_answer_it_asked_for():
     after = code[loop:code.index("if (a.behind_tc) pdl_wait();", loop)]
     failed = after[after.rindex("if (!ok)"):]
     assert re.search(r"mbar_wait_bounded\(&answered, ", failed), failed
+
+
+def test_a_meeting_that_runs_out_is_not_passed_over():
+    """Warps that edit a tile together may not go on as if the others had come: the wait flags the status, as every other one does."""
+    code = _code("shared_stream.cuh")
+    body = code[code.index("auto sync_set ="):]
+    body = body[:body.index("\n                };")]
+    assert "mbar_wait_bounded" not in body and re.search(r"\bwait\(&meet\[set\], ", body), body
