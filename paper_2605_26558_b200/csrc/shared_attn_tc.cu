@@ -27,6 +27,7 @@ struct StShape {
     static constexpr int q_tile = kStTile * D * 2;       // Q of 128 pairs; K or V of 128 positions: boxes of 128 x 64, 128-byte swizzle
     static constexpr int slots = D == 128 ? 5 : 8;
     static constexpr int smem = (2 + slots) * q_tile + 256 + 1024;
+    static_assert((2 * slots + 6) * 8 + 4 <= 256, "the barriers behind the ring");
     static_assert(slots * q_tile >= 8 * 32 * D * 4, "the outputs pass through the ring");
     static_assert(smem <= (int)kSmemPerBlock, "shared memory of a CTA");
 };
@@ -93,8 +94,8 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
     uint8_t* base = reinterpret_cast<uint8_t*>(((uintptr_t)smem_dyn + 1023) & ~(uintptr_t)1023);
     uint8_t *sQ = base, *sT = base + 2 * kTile;
     uint64_t* full = reinterpret_cast<uint64_t*>(sT + S::slots * kTile);
-    uint64_t *empty = full + S::slots, *s_full = empty + S::slots, *p_done = s_full + 2, *o_full = p_done + 2;
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(o_full + 1);
+    uint64_t *empty = full + S::slots, *s_full = empty + S::slots, *p_done = s_full + 2, *o_full = p_done + 2, *drained = o_full + 1;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(drained + 1);
     int64_t* s_q = reinterpret_cast<int64_t*>(sT + (S::slots - 1) * kTile);      // where a pair's query lies, -1: there is none; before the slot's first tile
     const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
     // ---- which pairs, which positions ----
@@ -110,6 +111,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
         for (int b = 0; b < S::slots; ++b) { mbar_init(&full[b], 1); mbar_init(&empty[b], 1); }
         for (int b = 0; b < 2; ++b) { mbar_init(&s_full[b], 1); mbar_init(&p_done[b], 4); }
         mbar_init(o_full, 1);
+        mbar_init(drained, 1);
         fence_mbar_init();
     }
     if (warp == 1) {
@@ -252,6 +254,8 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
                     for (int s = it; s < it + S::slots; ++s)                     // what is in flight lands before the CTA ends (bounded)
                         mbar_wait_bounded(&full[s % S::slots], (uint32_t)(s / S::slots) & 1u);
                 }
+                tc_commit(drained);                      // also who gives up, and whoever gives up beside it: tensor memory is freed behind the last product
+                mbar_wait_bounded(drained, 0);
             }
         }
     } else {

@@ -25,3 +25,12 @@ def test_a_meeting_that_runs_out_is_not_passed_over():
     body = code[code.index("auto sync_set ="):]
     body = body[:body.index("\n                };")]
     assert "mbar_wait_bounded" not in body and re.search(r"\bwait\(&meet\[set\], ", body), body
+
+
+def test_tensor_memory_is_freed_behind_the_products():
+    """Whether its waits ran out or not, the thread that issued products waits for the last of them before its block frees tensor memory."""
+    code = _code("shared_attn_tc.cu")
+    issue = code[code.index("if (tc_elect()) {"):code.index("} else {\n        asm volatile(\"setmaxnreg.inc")]
+    end = issue[issue.rindex("tc_commit("):]
+    assert re.search(r"tc_commit\((\w+)\);\s*mbar_wait_bounded\(\1, 0\);", end), end
+    assert "if (ok)" not in end.split("mbar_wait_bounded")[0], end
