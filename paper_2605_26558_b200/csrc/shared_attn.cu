@@ -41,8 +41,8 @@ __global__ void __launch_bounds__(merge_threads(WARPS)) k_shared_merge(SharedAtt
     SaParts first, second;
     const int all = b * P + p, seg = p >> seg_shift, in_seg = p & ((1 << seg_shift) - 1);        // the pair among those of all sequences; its segment
     int2 pre = make_int2(0, -1), own = make_int2(0, -1);
-    if (a.p_groups) pre = a.slots[(all >> seg_shift) * a.n_kv + head];
-    if (n > 0) own = a.slots[a.p_groups * a.n_kv + (b * a.c_groups + seg) * a.n_kv + head];
+    if (a.p_groups) pre = shared_slots(a.slots[(all >> seg_shift) * a.n_kv + head], a.n_slots);
+    if (n > 0) own = shared_slots(a.slots[a.p_groups * a.n_kv + (b * a.c_groups + seg) * a.n_kv + head], a.n_slots);
     if (a.prefix && !a.p_groups) {
         const bool two = all / (2 * kStTile) < a.pre_n2;
         const int64_t at = two ? ((int64_t)head * a.pre_n2 + all / (2 * kStTile)) * 2 * kStTile + all % (2 * kStTile)
@@ -263,6 +263,7 @@ static int shared_plan(const cass_cache_geom* c, const cass_shared_attn* t, bool
     size_t off = 0;
     auto take = [&](size_t b) { const size_t o2 = off; off = align_up(off + b, 256); return o2; };
     const size_t segments = (size_t)a.n_kv * ((size_t)a.p_groups + (size_t)a.n_seq * a.c_groups), slots = (size_t)kSaLevels * a.ctas + segments;
+    a.n_slots = (int)slots;
     plan->at_o = take(slots * a.pairs * a.d * 4);
     plan->at_ml = take(slots * a.pairs * 8);
     plan->at_slots = take(segments * 8);

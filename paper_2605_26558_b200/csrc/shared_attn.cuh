@@ -66,6 +66,7 @@ struct SharedAttn {
     float* part_o;                                       // [slot][pairs][d]
     float2* part_ml;                                     // [slot][pairs]
     int2* slots;                                         // [segment]: the first and the last slot of the streaming kernel's parts
+    int n_slots;                                         // that part_o and part_ml have
     float* scores;                                       // [sequence][KV head][pair][score_stride], for the weights; or null
     int64_t score_stride;                                // the capacity, rounded up to 4
     float* lse;                                          // [sequence][KV head][pair], in powers of two, for the weights
@@ -122,6 +123,8 @@ __device__ __forceinline__ int shared_span(const SaList& s, int w) { return w >=
 __device__ __forceinline__ int shared_cut(const SaList& s, int tiles, int level) {       // tiles of a span before its piece `level`
     return level == 0 ? 0 : level >= s.levels ? tiles : level == 1 ? tiles - tiles / 4 : tiles - max(tiles / 16, 1);
 }
+// What the table says of a segment's parts; none, if it says what cannot be (the streaming kernel gave up before it wrote it).
+__host__ __device__ __forceinline__ int2 shared_slots(int2 s, int n) { return s.x >= 0 && s.x <= s.y && s.y < n ? s : make_int2(0, -1); }
 constexpr int64_t kSaMaxTiles = 1 << 30;
 
 // CTAs of the streaming kernel that an SM holds.

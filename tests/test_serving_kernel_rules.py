@@ -34,3 +34,38 @@ def test_tensor_memory_is_freed_behind_the_products():
     end = issue[issue.rindex("tc_commit("):]
     assert re.search(r"tc_commit\((\w+)\);\s*mbar_wait_bounded\(\1, 0\);", end), end
     assert "if (ok)" not in end.split("mbar_wait_bounded")[0], end
+
+
+# Ranges of parts as the table may hold them: written, never written (whatever the scratch held), half written.
+_SLOTS = r"""
+#include <cstdio>
+#include <random>
+#include "shared_attn.cuh"
+int main() {
+    std::mt19937 rng(1);
+    long kept = 0, bad = 0, cut = 0;
+    for (int n : {1, 2, 450, 1 << 20})
+        for (int i = 0; i < 100000; ++i) {
+            int2 s = make_int2((int)rng(), (int)rng());
+            if (i % 3 == 0) s = make_int2((int)(rng() % n), (int)(rng() % n));
+            if (i % 1000 == 1) s = make_int2(0, n - 1);
+            if (i % 1000 == 2) s = make_int2(0, n);
+            if (i % 1000 == 4) s = make_int2(-1, 0);
+            const int2 t = cass::shared_slots(s, n);
+            const bool fine = s.x >= 0 && s.y < n && s.x <= s.y;
+            if (fine ? t.x != s.x || t.y != s.y : t.y - t.x + 1 != 0 || t.x < 0) ++bad;
+            ++(fine ? kept : cut);
+        }
+    std::printf("%ld %d %d\n", bad, kept > 1000, cut > 1000);
+}
+"""
+
+
+def test_parts_that_were_never_written_are_not_read(tmp_path):
+    """The merge reads where a segment's parts lie from the scratch.  If the kernel before it gave up, that is whatever was there: a range
+    outside the parts counts as none."""
+    import test_first_calls
+    assert test_first_calls._output(tmp_path, _SLOTS) == ["0", "1", "1"]
+    code = _code("shared_attn.cu")
+    reads = re.findall(r"[^;]*\ba\.slots\[[^;]*;", code)
+    assert reads and all("shared_slots(" in r for r in reads), reads
