@@ -22,9 +22,10 @@ def test_a_block_that_gives_up_waits_for_the_answer_it_asked_for():
 def test_a_meeting_that_runs_out_is_not_passed_over():
     """Warps that edit a tile together may not go on as if the others had come: the wait flags the status, as every other one does."""
     code = _code("shared_stream.cuh")
-    body = code[code.index("auto sync_set ="):]
-    body = body[:body.index("\n                };")]
-    assert "mbar_wait_bounded" not in body and re.search(r"\bwait\(&meet\[set\], ", body), body
+    body = code[code.index("auto meeting ="):]
+    assert re.search(r"if \(!mbar_wait_bounded\(&meet\[set\], phase\)\) met = false;", body[:body.index("\n                };")]), body[:400]
+    last = body[body.index("meeting(1);"):]
+    assert re.search(r"!__all_sync\(0xffffffffu, met\)\) \{\s*ok = false;[^}]*CASS_ERR_TIMEOUT", last[:500]), last[:500]
 
 
 def test_tensor_memory_is_freed_behind_the_products():
