@@ -443,7 +443,7 @@ int cass_shared_prefix_attention(const cass_cache_geom* cache, const cass_shared
  * weight: fp32 [n_seq][n_kv_heads][capacity]; lens: int32 [n_seq].  kept: int32 [n_seq][n_kv_heads][budget], the positions that
  * stay, ascending, then -1; new_lens: int32 [n_seq] = min(lens, budget), may be lens.  cache_out NULL: in place (k_out and v_out
  * NULL too); otherwise K and V go to another cache of the same type, heads and sequences and a capacity of at least
- * `budget`, which must not overlap the first.  weight_out (optional, may be `weight` in place): fp32 [n_seq][n_kv_heads]
+ * `budget`, which must not overlap the first.  What K and V are written to must not overlap (the same pointer: CASS_ERR_INVALID_ARG).  weight_out (optional, may be `weight` in place): fp32 [n_seq][n_kv_heads]
  * [capacity of the output], the weights of what stays, then zeros up to the capacity.  Rows of K and V behind what stays are left as
  * they were.  A sequence whose length is outside 0 .. capacity is left alone: its `kept` is -1, its new_lens its length, its
  * caches and weights are not written.

@@ -332,6 +332,7 @@ extern "C" int cass_kv_evict(const cass_cache_geom* cache, void* k_cache, void* 
     if (budget < 1 || budget > o.capacity || n_first < 0 || n_last < 0 || n_first > budget || n_last > budget - n_first) return CASS_ERR_INVALID_ARG;
     if (in_place) { k_out = k_cache; v_out = v_cache; }
     else if (k_out == k_cache || v_out == v_cache || k_out == v_cache || v_out == k_cache) return CASS_ERR_INVALID_ARG;
+    if (k_out == v_out) return CASS_ERR_INVALID_ARG;     // two CTAs would move the same rows
     if (((uintptr_t)k_cache | (uintptr_t)v_cache | (uintptr_t)k_out | (uintptr_t)v_out) & 15) return CASS_ERR_INVALID_ARG;
     if (((uintptr_t)weight | (uintptr_t)weight_out | (uintptr_t)lens | (uintptr_t)kept | (uintptr_t)new_lens) & 3) return CASS_ERR_INVALID_ARG;
     if (weight_out == weight && o.capacity != g.capacity && g.n_seq * (int64_t)g.n_kv_heads > 1) return CASS_ERR_INVALID_ARG;

@@ -79,3 +79,11 @@ def test_tensors_of_other_types_are_refused(cass):
             {2: [half, f32], 3: [half], 6: [half], 7: [i64], 8: [f32], 9: [f64, half], 10: [f64], 11: [bf], 14: [i64]})
     refused(cass.cass_kv_evict, [cache, bf, bits, f32, i32, 1, 0, 0, cache, bf, bf, f32, i32, i32],
             {1: [half], 2: [f32], 3: [f64], 4: [i64], 9: [half], 11: [bf], 12: [i64], 13: [i64]})
+
+
+def test_an_eviction_of_keys_and_values_in_one_place_is_refused(cass):
+    """Both would be moved over one another.  (Read from one place and written to two, they may be the same.)"""
+    c, out = (cass.CacheGeom(cass.BF16, 1, 1, 8, n, 0, 8, 0) for n in (100, 50))
+    p = lambda i: C.c_void_p(AT + (i << 24))  # noqa: E731
+    assert cass.lib.cass_kv_evict(C.byref(c), p(0), p(0), p(2), p(3), 50, 0, 0, None, None, None, None, p(4), p(5), None) == cass.ERR_INVALID_ARG
+    assert cass.lib.cass_kv_evict(C.byref(c), p(0), p(1), p(2), p(3), 50, 0, 0, C.byref(out), p(6), p(6), None, p(4), p(5), None) == cass.ERR_INVALID_ARG
