@@ -28,7 +28,6 @@ template <> struct SaType<CASS_BF16> {
     static constexpr float kGrowth = 8.f;                // powers of two that numerators may grow over their base before what was summed is rescaled
     static constexpr float kLift = 0.f;                  // of numerators that are rescaled at every new maximum
     static __device__ __forceinline__ float get(uint32_t v) { return __uint_as_float(v << 16); }
-    static __device__ __forceinline__ uint16_t put(float v) { return float_to_bf16_bits(v); }
 };
 template <> struct SaType<CASS_F16> {
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) {
@@ -44,7 +43,6 @@ template <> struct SaType<CASS_F16> {
     static constexpr float kGrowth = 4.f;                // (with 8, and no lift: 64 sequences of 40 heads behind 32768 positions 90.3 us, so 92.8)
     static constexpr float kLift = 15.f;
     static __device__ __forceinline__ float get(uint32_t v) { return __half2float(__ushort_as_half((uint16_t)v)); }
-    static __device__ __forceinline__ uint16_t put(float v) { return __half_as_ushort(__float2half_rn(v)); }
 };
 
 __device__ __forceinline__ float exp2_fast(float x) {
@@ -96,11 +94,11 @@ __device__ __forceinline__ int shared_len(const SharedAttn& a, int b) {
 
 // The streaming kernel's segments are numbered: those of the prefix (group, head), then those of the sequences (sequence, group,
 // head); their tiles form one list, cut into as many even spans as CTAs fit the GPU (a tile at least).  SMs do not get the same share of the
-// memory's rate (of equal spans of one cache of 32000 positions the first ends 21 us after the start, the last 30), so a span is cut again,
-// into 3/4, 3/16 and 1/16 of it where it has 16 tiles (3/4 and 1/4 where it has 4, not at all below), and the CTAs take first the large
-// pieces, then, as they get free, the small ones.  (Small pieces at the
-// list's end instead leave the last segment with hundreds of parts.)  Pieces are numbered along the list, and the part of piece u that lies
-// in segment s goes to slot u + s (from one part to the next either number grows, so no two share a slot).
+// memory's rate (of equal spans of one cache of 32000 positions the first ends 21 us after the start, the last 30), so a span is cut again: from
+// 8 tiles on a quarter is left for later and a sixteenth of it (a tile at least) for last, from 4 on a quarter; below that it is one piece.
+// The CTAs take first the large pieces, then, as they get free, the small ones.  (Small pieces at the list's end instead leave the last
+// segment with hundreds of parts.)  Pieces are numbered along the list, and the part of piece u that lies in segment s goes to slot u + s (from
+// one part to the next either number grows, so no two share a slot).
 constexpr int kSaLevels = 3;
 __host__ __device__ inline int shared_levels(int each) { return each >= 8 ? 3 : each >= 4 ? 2 : 1; }         // pieces of a span, none of them empty
 struct SaList {

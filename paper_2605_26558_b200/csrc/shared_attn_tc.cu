@@ -61,18 +61,6 @@ __device__ __forceinline__ void st_st32(uint32_t taddr, const uint32_t* v) {
         "r"(v[21]), "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31])
         : "memory");
 }
-__device__ __forceinline__ float st_exp2(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
-template <int DT>
-__device__ __forceinline__ uint32_t st_pack(float lo, float hi) {
-    uint32_t r;
-    if (DT == CASS_BF16) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
 // kind::f16, D fp32, A and B of type DT; b_mn_major: B is stored with its columns contiguous
 template <int DT>
 constexpr uint32_t st_idesc(int m, int n, bool b_mn_major) {
@@ -284,7 +272,7 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
             const float top = fmaxf(fmaxf(x[0], x[1]), fmaxf(x[2], x[3])) * a.scale_log2;      // (the scale is positive)
             const bool grew = top > m + T::kGrowth;       // also from -inf
             if (__any_sync(0xffffffffu, grew)) {
-                const float fix = grew ? st_exp2(m - top) : 1.f;
+                const float fix = grew ? exp2_fast(m - top) : 1.f;
                 if (grew) m = top;
                 if (u > 0) {
                     l *= fix;
@@ -307,10 +295,10 @@ __global__ void __launch_bounds__(kStThreads, 1) k_shared_prefix_tc(const __grid
                 uint32_t b[32];
 #pragma unroll
                 for (int e = 0; e < 64; e += 2) {
-                    const float p0 = st_exp2(fmaf(s[c + e], a.scale_log2, -from)), p1 = st_exp2(fmaf(s[c + e + 1], a.scale_log2, -from));
+                    const float p0 = exp2_fast(fmaf(s[c + e], a.scale_log2, -from)), p1 = exp2_fast(fmaf(s[c + e + 1], a.scale_log2, -from));
                     sum[e & 2] += p0;
                     sum[(e & 2) + 1] += p1;
-                    b[e / 2] = st_pack<DT>(p0, p1);
+                    b[e / 2] = T::pack(p0, p1);
                 }
                 st_st32(sc + c / 2, b);
             }
@@ -369,6 +357,7 @@ int64_t shared_tc_plan(SharedAttn& a) {
     // CTAs over the positions: the least time of the slower kind with at most one CTA an SM (if there are not more heads and pairs
     // than that anyway).  A tile of positions takes two tiles of pairs 2.1 us (the products, 1.2 PFLOP/s), one tile 1.3 (K and V at the
     // memory's rate); an output to be left behind 3.
+    // (Measured for head size 128.  For 64 products, bytes and outputs are half of it, the exponentials are not; the choice is taken alike.)
     // SMs are left to the streaming kernel, which starts beside this one: the products do not need the memory's rate that the caches do.
     // Their share is what that kernel's tiles take, 0.6 us each (1.5 with more than 16 pairs), if the caches are 3/4 full, half at most; and
     // half where there is little to do, as each SM more saves less than the parts that it leaves cost.  64 sequences (40 heads) behind
