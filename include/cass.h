@@ -391,11 +391,11 @@ typedef struct cass_rope_geom {
 
 /* Turns every pair (a, b) of row r's heads by t = positions[r] * f_j: (g (a cos t - b sin t), g (a sin t + b cos t)), g the factor
  * behind the frequencies; values beyond rot_dim are copied.  transpose: by -t, which is the gradient of the forward call's
- * inputs from that of its outputs and, for g = 1, undoes the rotation.  Angles are formed in 64 bits (any int32 position), the
- * products in 32, one rounding at the end.  positions: device int32 [rows], or NULL for 0, 1, 2, ...  k may be NULL
+ * inputs from that of its outputs and, for g = 1, undoes the rotation.  Angles are formed in 64 bits (any int32 position; off by
+ * a few 2^-53 of themselves), the products in 32, one rounding at the end.  positions: device int32 [rows], or NULL for 0, 1, 2, ...  k may be NULL
  * (n_k_heads = 0), and q likewise.  q_out = q with the same strides rotates in place (k likewise); outputs overlap neither
- * each other nor inputs otherwise.  The elements of one output must not overlap (CASS_ERR_INVALID_ARG).  rows = 0 does nothing.
- * Calls for rows x heads up to 2^31 - 1. */
+ * each other nor inputs otherwise.  The elements of one output must not overlap (CASS_ERR_INVALID_ARG).  rows = 0 does nothing, and needs
+ * no addresses.  rot_dim up to 4096, 65535 heads, rows x heads up to 2^31 - 1; CASS_ERR_UNSUPPORTED otherwise. */
 int cass_rope(const cass_rope_geom* geom, const double* freqs, const int32_t* positions, int rows, const void* q, const void* k,
               void* q_out, void* k_out, int transpose, void* stream);
 
@@ -408,8 +408,9 @@ typedef struct cass_cache_geom {
     int64_t seq_stride, pos_stride, head_stride;
 } cass_cache_geom;
 
-/* Grouped-query attention of `rows` new rows of every sequence (1 to 16) over a prefix that all sequences share, read once
- * for all of them, and each sequence's own cache.  K of both is post-RoPE.  With lens[b] the positions in sequence b's cache,
+/* Grouped-query attention of `rows` new rows of every sequence (1 to 16) over a prefix that all sequences share and each
+ * sequence's own cache.  A KV head's prefix is read once for 256 (sequence, row, query head) pairs with head sizes 64 and 128, for 32 or 64
+ * with 32 and 96, for 16 with 192 and 256.  K of both is post-RoPE.  With lens[b] the positions in sequence b's cache,
  * the new rows' among them, row r sees the whole prefix and the first lens[b] - (rows - 1 - r) positions of its cache:
  *   s = scale q.k;  out = sum_j softmax(s)_j v_j;  lse = ln sum_j e^{s_j}  (-inf, and out 0, for a row that sees nothing)
  * What a row does not see does not reach its results, whatever its bits.  A sequence with lens[b] < 0 is not there: nothing
@@ -420,7 +421,8 @@ typedef struct cass_cache_geom {
  * q, out: dtype of the cache, 16-byte aligned, strides multiples of 8.  lse (optional): fp32 [n_seq][rows][n_q_heads].
  * prefix_len = 0 (pointers NULL) or capacity = 0 (pointers and lens NULL: every row sees the prefix alone) leave a part out.
  * head_dim 32, 64, 96, 128, 192 or 256; at most 16 query heads a KV head and 1024 in all; n_seq up to 1024; CASS_ERR_UNSUPPORTED otherwise.
- * Probabilities are rounded to the cache's type for the second product, sums are 32 bits.  Results are the same bits
+ * Probabilities are rounded to the cache's type for the second product (half a step of each; those of a long flat tail keep their bits
+ * in fp16 too), sums are 32 bits.  Results are the same bits
  * on every call with the same inputs and sizes.  scratch: device, 16-byte aligned, of cass_shared_prefix_scratch_bytes; two calls
  * that may overlap on the GPU need their own.  d_status (required): device int32, left alone if nothing
  * went wrong (also CASS_ERR_TIMEOUT: a bounded device wait ran out, results are undefined). */

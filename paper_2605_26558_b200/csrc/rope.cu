@@ -1,9 +1,10 @@
 // Rotary positions of queries and keys in the caller's layout: y = g (cos t, -sin t; sin t, cos t) (a, b) for every pair of a head,
 // t = position * frequency of the pair.
 // Bound: memory (each value read and written once).  A CTA takes the rows whose sines and cosines its threads form in one go, one
-// (row, pair) a thread: the angle in 64 bits, reduced there to a quarter turn, then sincospif of at most 1/4, so that far positions
-// are as exact as near ones and no table bounds the positions.  All heads of the row share them through shared memory; a thread's
-// values travel while they are formed.  8191 rows of 40 half-rotated heads of 128 into other tensors 28.6 us, 5.9 TB/s, 90 % of a copy's
+// (row, pair) a thread: the angle in 64 bits, reduced there to a quarter turn, then sincospif of at most 1/4, so that no table bounds the
+// positions.  The product with the frequency (itself rounded, of a power good to a unit or two), and that with 1 / pi, are off by a few 2^-53 of the
+// angle: less than the sine's own 2^-24 up to some 2^27 radians, up to 2^-20 at 2^31.  All heads of the row share them
+// through shared memory; a thread's values travel while they are formed.  8191 rows of 40 half-rotated heads of 128 into other tensors 28.6 us, 5.9 TB/s, 90 % of a copy's
 // rate; the gradient of 32768 fp32 rows of 48 heads 234 us, 6.9 TB/s, a little above a copy's.
 #include <cmath>
 #include <cuda_fp16.h>

@@ -1,5 +1,5 @@
 // Attention of a batch behind a shared prefix.  All sequences' queries of a KV head form the rows of one product with the prefix,
-// which is read once; every sequence's own cache is read by its own queries.  Both leave partial results (output, maximum, sum) that
+// which is read once for 16 to 256 of them; every sequence's own cache is read by its own queries.  Both leave partial results (output, maximum, sum) that
 // k_shared_merge joins; the weights that the caches' positions got follow from the scores, once the sums are known.
 //
 // The prefix behind few queries and the caches are shared_stream.cuh's, the prefix behind many is shared_attn_tc.cu's.
