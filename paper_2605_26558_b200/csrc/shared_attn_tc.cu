@@ -8,7 +8,7 @@
 // pairs each has one, and both use the same K and V; with one they take the positions' tiles in turn.  While one's numerators are formed
 // the other's products run.
 // Bound: with one tile of pairs K and V bytes, 1.31 us for the 64 KB of 128 positions on every SM, 7.4 TB/s.  With two, the chain of
-// a tile (scores, softmax, product): the two warpgroups' chains overlap, but tensor pipe (54 % of the clocks) and exponentials (16 a clock: 1024
+// a tile (scores, softmax, product): the two warpgroups' chains overlap, but tensor pipe (54 % of the clocks, fp16 52) and exponentials (16 a clock: 1024
 // clocks a tile, as both products take) are each busy half of the time; 2.1 us for the four products, 1.18 PFLOP/s, 73 % of a library
 // product's rate.  The positions' tiles by halves of 64 took 2.45 us, four softmax warpgroups of 64 columns 2.25.
 #include "tc.cuh"
